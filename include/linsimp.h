@@ -206,6 +206,75 @@ int linsimp_decode_chunk(int64_t S, int32_t H, int32_t T, int32_t D, int32_t Dv,
                          float* a, float* rho, void* ring_r, void* ring_u, int64_t* pos, void* out,
                          void* stream);
 
+/* ---- The mixers that a LinSimp stack interleaves with ----
+ *
+ * Softmax attention (the layers between the LinSimp layers of the paper's
+ * Attn+LinSimp models, Sec. 4), behind the conventions
+ * above: dense [B, heads, rows, D] device tensors, 16-byte aligned, the
+ * caller's workspace (256-byte aligned), calls that only enqueue on `stream`,
+ * negative statuses.  D is 32, 64 or 128 with LINSIMP_BF16 and 32 or 64 with
+ * LINSIMP_F32.  Results are the same bits on every run of a call. */
+
+typedef struct {
+  int64_t B;       /* batch (sequences)                                       */
+  int64_t H;       /* query heads                                             */
+  int64_t Hkv;     /* heads of k and v; H is a multiple, head h reads h / (H / Hkv) */
+  int64_t nq;      /* rows of q, out                                          */
+  int64_t nk;      /* rows of k, v (the slots of the ring in linsimp_attn_step) */
+  int64_t window;  /* > 0 (with causal): a query sees the last `window` keys  */
+  int32_t D;       /* width of q, k, v, out                                   */
+  int32_t dtype;   /* linsimp_dtype                                           */
+  int32_t causal;  /* 1: no query sees a later key; 0: every key              */
+  float scale;     /* > 0; D^-1/2 in the usual layer                          */
+} linsimp_attn_dims;
+
+/* Bytes of workspace linsimp_attn_fwd or linsimp_attn_step (for_backward = 0)
+ * or linsimp_attn_bwd (1; enough for the forward too) needs.  0 for invalid or
+ * unsupported dims. */
+size_t linsimp_attn_workspace_size(const linsimp_attn_dims* dims, int for_backward);
+
+/* Softmax attention, forward:
+ *   out_i = sum_j p_ij v_j,  p_ij = exp(scale q_i . k_j - lse_i)
+ *   q : [B, H, nq, D]   k, v : [B, Hkv, nk, D]   out : [B, H, nq, D], written
+ *   lens_q, lens_k : [B] int32 on the device, or NULL (nq, nk): the rows of each
+ *         sequence that exist; values outside [0, nq] ([0, nk]) are taken as the
+ *         nearest end.  Rows of k and v past lens_k are never used, whatever
+ *         they hold; rows of out past lens_q are written as zeros.
+ *   lse : [B, H, nq] float32 (natural logarithm), or NULL; the backward needs it
+ * The last query sits at the last key: query i of a sequence with lq queries
+ * and lk keys has position i + lk - lq, and with causal sees keys up to that
+ * position (with a window, the last `window` of them).  So nq = nk is a
+ * training step or a prompt, nq < nk a continuation against cached keys.  A
+ * row that sees no key has out = 0, lse = -inf and no gradient. */
+int linsimp_attn_fwd(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
+                     const int32_t* lens_q, const int32_t* lens_k, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward: exact gradient of sum(dout * out), the probabilities recomputed
+ * from lse.
+ *   q, k, v, lens_q, lens_k : as passed to the forward;  out, lse : what it wrote
+ *   dout : [B, H, nq, D] dtype
+ *   dq : [B, H, nq, D];  dk, dv : [B, Hkv, nk, D], summed over the query heads
+ *        that share a key head; overwritten, zeros in rows that do not exist. */
+int linsimp_attn_bwd(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
+                     const int32_t* lens_q, const int32_t* lens_k, const void* out,
+                     const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                     void* workspace, size_t workspace_bytes, void* stream);
+
+/* One decode step for B sequences on a ring of nk slots: token pos[b] is written
+ * into slot pos[b] mod nk of kcache, vcache, and its queries attend to the
+ * min(pos[b] + 1, nk) tokens in the ring, itself included (a ring of w slots is
+ * a window of w tokens; a longer prompt is its last nk tokens, each in slot
+ * position mod nk).  Slots that hold no token do not affect the result.
+ *   dims : nq = 1, nk = slots, window = 0 (causal is not read)
+ *   q : [B, H, D]   k, v : [B, Hkv, D]   out : [B, H, D]
+ *   kcache, vcache : [B, Hkv, nk, D] in/out
+ *   pos : [B] int64, not changed (one tensor serves all layers); a negative
+ *         value leaves the sequence's cache alone and gives a zero out. */
+int linsimp_attn_step(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
+                      void* kcache, void* vcache, const int64_t* pos, void* out, void* workspace,
+                      size_t workspace_bytes, void* stream);
+
 /* Per-kernel timing, for tuning and roofline reports.  While enabled
  * (on != 0), every kernel the library launches is bracketed by two HIP events
  * recorded on its stream; enabling costs two event records per launch and

@@ -190,6 +190,34 @@ int check_states(const void* ws, const Shape& s, const void* k, const void* v, c
   return LINSIMP_E_INVALID_ARG;
 }
 
+bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
+
+int check_ptrs(const char* names, const void* const* ps, int np) {
+  for (int i = 0; i < np; ++i) {
+    if (ps[i] == nullptr) {
+      set_error("argument %d of (%s) is NULL", i, names);
+      return LINSIMP_E_INVALID_ARG;
+    }
+    if (!aligned16(ps[i])) {
+      set_error("argument %d of (%s) is not 16-byte aligned", i, names);
+      return LINSIMP_E_INVALID_ARG;
+    }
+  }
+  return LINSIMP_OK;
+}
+
+int check_buf(const char* what, const void* p, size_t bytes, size_t need) {
+  if (p == nullptr || ((uintptr_t)p & 255) != 0) {
+    set_error("%s must be a non-NULL 256-byte aligned device pointer", what);
+    return LINSIMP_E_WORKSPACE;
+  }
+  if (bytes < need) {
+    set_error("%s too small: %zu bytes given, %zu needed", what, bytes, need);
+    return LINSIMP_E_WORKSPACE;
+  }
+  return LINSIMP_OK;
+}
+
 bool shape_supported(const Shape& s, bool /*backward*/) {
   if (s.w < 1 || s.w > 128) return false;
   if (!wide_window_ok(s.dtype, s.D, s.m, (s.w + 31) / 32)) return false;
@@ -200,8 +228,6 @@ bool shape_supported(const Shape& s, bool /*backward*/) {
 }  // namespace linsimp
 
 using namespace linsimp;
-
-static bool aligned16(const void* p) { return ((uintptr_t)p & 15) == 0; }
 
 // Validates dims; fills `s`.  Returns LINSIMP_OK or an error status.
 static int check_dims(const linsimp_dims* d, Shape* s, bool backward, bool bh_on_grid_y = true) {
@@ -240,20 +266,6 @@ static int check_decode_grid(int64_t S, int32_t H, int32_t m) {
     set_error("decode: S*H = %lld (sequence, head) pairs, at most %lld per call at m = %d",
               (long long)(S * (int64_t)H), (long long)most, m);
     return LINSIMP_E_UNSUPPORTED;
-  }
-  return LINSIMP_OK;
-}
-
-static int check_ptrs(const char* names, const void* const* ps, int np) {
-  for (int i = 0; i < np; ++i) {
-    if (ps[i] == nullptr) {
-      set_error("argument %d of (%s) is NULL", i, names);
-      return LINSIMP_E_INVALID_ARG;
-    }
-    if (!aligned16(ps[i])) {
-      set_error("argument %d of (%s) is not 16-byte aligned", i, names);
-      return LINSIMP_E_INVALID_ARG;
-    }
   }
   return LINSIMP_OK;
 }
@@ -557,18 +569,6 @@ int check_head(const linsimp_dims* dims, const linsimp_head_opts* opts, Shape* s
   if (!okw) {
     set_error("head: D=%d Dv=%d not in {32, 64, 128}", s->D, s->Dv);
     return LINSIMP_E_UNSUPPORTED;
-  }
-  return LINSIMP_OK;
-}
-
-int check_buf(const char* what, const void* p, size_t bytes, size_t need) {
-  if (p == nullptr || ((uintptr_t)p & 255) != 0) {
-    set_error("%s must be a non-NULL 256-byte aligned device pointer", what);
-    return LINSIMP_E_WORKSPACE;
-  }
-  if (bytes < need) {
-    set_error("%s too small: %zu bytes given, %zu needed", what, bytes, need);
-    return LINSIMP_E_WORKSPACE;
   }
   return LINSIMP_OK;
 }

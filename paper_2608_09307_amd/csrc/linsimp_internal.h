@@ -116,6 +116,10 @@ inline int64_t kernel_slots(K kernel, int threads) {
 }
 
 void set_error(const char* fmt, ...);
+// argument checks of the C ABI: 0, or a negative linsimp status with the message set
+bool aligned16(const void* p);
+int check_ptrs(const char* names, const void* const* ps, int np);
+int check_buf(const char* what, const void* p, size_t bytes, size_t need);
 bool shape_supported(const Shape& s, bool backward);
 
 }  // namespace linsimp

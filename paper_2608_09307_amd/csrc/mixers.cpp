@@ -1,0 +1,164 @@
+// C ABI of softmax attention: argument
+// validation, workspace carving and dispatch.  Contracts: include/linsimp.h.
+#include "../../include/linsimp.h"
+
+#include <math.h>
+
+#include "attn.h"
+#include "linsimp_internal.h"
+
+using namespace linsimp;
+
+namespace {
+
+size_t al(size_t x) { return (x + 255) & ~(size_t)255; }
+
+int check_width(const char* what, int D, int dtype) {
+  if (dtype != LINSIMP_F32 && dtype != LINSIMP_BF16) {
+    set_error("%s: dtype %d is not LINSIMP_F32 or LINSIMP_BF16", what, dtype);
+    return LINSIMP_E_INVALID_ARG;
+  }
+  if (!(D == 32 || D == 64 || (D == 128 && dtype == LINSIMP_BF16))) {
+    set_error("%s: D=%d is not 32, 64 or (bf16) 128", what, D);
+    return LINSIMP_E_UNSUPPORTED;
+  }
+  return LINSIMP_OK;
+}
+
+// an optional pointer (NULL, or aligned)
+int check_opt(const char* name, const void* p, uintptr_t mask) {
+  if (((uintptr_t)p & mask) == 0) return LINSIMP_OK;
+  set_error("%s is not %d-byte aligned", name, (int)mask + 1);
+  return LINSIMP_E_INVALID_ARG;
+}
+
+int check_attn(const linsimp_attn_dims* d, AttnShape* s) {
+  if (d == nullptr) { set_error("dims is NULL"); return LINSIMP_E_INVALID_ARG; }
+  if (d->B < 1 || d->H < 1 || d->Hkv < 1 || d->nq < 1 || d->nk < 1) {
+    set_error("attn: sizes must be positive (B=%lld H=%lld Hkv=%lld nq=%lld nk=%lld)", (long long)d->B,
+              (long long)d->H, (long long)d->Hkv, (long long)d->nq, (long long)d->nk);
+    return LINSIMP_E_INVALID_ARG;
+  }
+  if (int rc = check_width("attn", d->D, d->dtype)) return rc;
+  if (d->H % d->Hkv != 0) {
+    set_error("attn: H=%lld is not a multiple of Hkv=%lld", (long long)d->H, (long long)d->Hkv);
+    return LINSIMP_E_INVALID_ARG;
+  }
+  if (d->causal != 0 && d->causal != 1) { set_error("attn: causal must be 0 or 1"); return LINSIMP_E_INVALID_ARG; }
+  if (d->window < 0 || (d->window > 0 && d->causal == 0)) {
+    set_error("attn: window must be >= 0, and 0 without causal");
+    return LINSIMP_E_INVALID_ARG;
+  }
+  if (!(d->scale > 0.0f) || !isfinite(d->scale)) {
+    set_error("attn: scale must be positive and finite");
+    return LINSIMP_E_INVALID_ARG;
+  }
+  // rows and slots are 32-bit within a head, and a grid has fewer than 2^32 threads
+  const int64_t big = (int64_t)1 << 30;
+  if (d->B > big || d->H > big || d->nq > big || d->nk > big || d->B * d->H > (int64_t)1 << 20 ||
+      d->B * d->H * d->nq > (int64_t)1 << 30 || d->B * d->Hkv * d->nk > (int64_t)1 << 38) {
+    set_error("attn: sizes too large: B*H=%lld (at most 2^20), B*H*nq (at most 2^30), nk (at most 2^30), "
+              "B*Hkv*nk (at most 2^38)", (long long)(d->B > big || d->H > big ? -1 : d->B * d->H));
+    return LINSIMP_E_UNSUPPORTED;
+  }
+  s->B = d->B; s->H = d->H; s->Hkv = d->Hkv; s->nq = d->nq; s->nk = d->nk;
+  s->window = d->window >= d->nk ? 0 : d->window;      // (no query then loses a key to it)
+  s->D = d->D; s->dtype = d->dtype; s->causal = d->causal; s->scale = d->scale;
+  return LINSIMP_OK;
+}
+
+// [ns][B][H][nq][D + 2] partial results, then (backward) delta [B][H][nq]
+size_t attn_ws(const AttnShape& s, int ns, bool backward, AttnArgs* a, void* base) {
+  const size_t rows = (size_t)s.B * s.H * s.nq;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    void* p = base ? (char*)base + off : nullptr;
+    off += al(bytes);
+    return (float*)p;
+  };
+  float* part = ns > 1 ? take((size_t)ns * rows * s.D * 4) : nullptr;
+  float* pml = ns > 1 ? take((size_t)ns * rows * 2 * 4) : nullptr;
+  if (backward) off = 0;                                 // the backward needs no partial results
+  float* delta = backward ? take(rows * 4) : nullptr;
+  if (a) { a->part = part; a->pml = pml; a->delta = delta; }
+  return off > 256 ? off : 256;
+}
+
+AttnArgs attn_args(const AttnShape& s) {
+  AttnArgs a{};
+  a.B = (int)s.B; a.H = (int)s.H; a.Hkv = (int)s.Hkv; a.G = (int)(s.H / s.Hkv);
+  a.nq = (int)s.nq; a.nk = (int)s.nk; a.causal = s.causal; a.window = (int)s.window;
+  a.ntq = (int)((s.nq + 127) / 128); a.ntk = (int)((s.nk + 127) / 128);
+  a.ns = 1; a.scale = s.scale; a.c = s.scale * 1.4426950408889634f;
+  return a;
+}
+
+}  // namespace
+
+extern "C" {
+
+size_t linsimp_attn_workspace_size(const linsimp_attn_dims* dims, int for_backward) {
+  AttnShape s;
+  if (check_attn(dims, &s) != LINSIMP_OK) return 0;
+  const size_t fwd = attn_ws(s, attn_splits(s), false, nullptr, nullptr);
+  const size_t bwd = for_backward ? attn_ws(s, 1, true, nullptr, nullptr) : 0;
+  return fwd > bwd ? fwd : bwd;
+}
+
+int linsimp_attn_fwd(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
+                     const int32_t* lens_q, const int32_t* lens_k, void* out, float* lse,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  AttnShape s;
+  int rc = check_attn(dims, &s);
+  if (rc) return rc;
+  const void* ps[] = {q, k, v, out};
+  if ((rc = check_ptrs("q,k,v,out", ps, 4))) return rc;
+  if ((rc = check_opt("lens_q", lens_q, 3)) || (rc = check_opt("lens_k", lens_k, 3)) || (rc = check_opt("lse", lse, 15)))
+    return rc;
+  const int ns = attn_splits(s);
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_ws(s, ns, false, nullptr, nullptr)))) return rc;
+  AttnArgs a = attn_args(s);
+  a.q = q; a.k = k; a.v = v; a.lens_q = lens_q; a.lens_k = lens_k; a.out = out; a.lse = lse; a.ns = ns;
+  attn_ws(s, ns, false, &a, workspace);
+  return launch_attn_fwd(s, a, (hipStream_t)stream);
+}
+
+int linsimp_attn_bwd(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
+                     const int32_t* lens_q, const int32_t* lens_k, const void* out,
+                     const float* lse, const void* dout, void* dq, void* dk, void* dv,
+                     void* workspace, size_t workspace_bytes, void* stream) {
+  AttnShape s;
+  int rc = check_attn(dims, &s);
+  if (rc) return rc;
+  const void* ps[] = {q, k, v, out, lse, dout, dq, dk, dv};
+  if ((rc = check_ptrs("q,k,v,out,lse,dout,dq,dk,dv", ps, 9))) return rc;
+  if ((rc = check_opt("lens_q", lens_q, 3)) || (rc = check_opt("lens_k", lens_k, 3))) return rc;
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_ws(s, 1, true, nullptr, nullptr)))) return rc;
+  AttnArgs a = attn_args(s);
+  a.q = q; a.k = k; a.v = v; a.lens_q = lens_q; a.lens_k = lens_k;
+  a.out = (void*)out; a.lse = (float*)lse; a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
+  attn_ws(s, 1, true, &a, workspace);
+  return launch_attn_bwd(s, a, (hipStream_t)stream);
+}
+
+int linsimp_attn_step(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
+                      void* kcache, void* vcache, const int64_t* pos, void* out, void* workspace,
+                      size_t workspace_bytes, void* stream) {
+  AttnShape s;
+  int rc = check_attn(dims, &s);
+  if (rc) return rc;
+  if (s.nq != 1 || dims->window != 0) {
+    set_error("attn step: nq must be 1 and window 0 (the ring's slots are the window)");
+    return LINSIMP_E_INVALID_ARG;
+  }
+  const void* ps[] = {q, k, v, kcache, vcache, pos, out};
+  if ((rc = check_ptrs("q,k,v,kcache,vcache,pos,out", ps, 7))) return rc;
+  const int ns = attn_splits(s);
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_ws(s, ns, false, nullptr, nullptr)))) return rc;
+  AttnArgs a = attn_args(s);
+  a.q = q; a.k = kcache; a.v = vcache; a.knew = k; a.vnew = v; a.pos = pos; a.out = out; a.ns = ns;
+  attn_ws(s, ns, false, &a, workspace);
+  return launch_attn_fwd(s, a, (hipStream_t)stream);
+}
+
+}  // extern "C"

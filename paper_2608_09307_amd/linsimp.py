@@ -34,6 +34,13 @@ class Dims(ctypes.Structure):
                 ("w", ctypes.c_int32), ("dtype", ctypes.c_int32), ("eps", ctypes.c_float)]
 
 
+class AttnDims(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("H", ctypes.c_int64), ("Hkv", ctypes.c_int64),
+                ("nq", ctypes.c_int64), ("nk", ctypes.c_int64), ("window", ctypes.c_int64),
+                ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("causal", ctypes.c_int32),
+                ("scale", ctypes.c_float)]
+
+
 class HeadOpts(ctypes.Structure):
     _fields_ = [("norm_eps", ctypes.c_float), ("rms_eps", ctypes.c_float), ("gate", ctypes.c_int32)]
 
@@ -45,7 +52,9 @@ BWD_REUSE_STATES = 1
 
 EXPORTS = ("linsimp_workspace_size", "linsimp_fwd", "linsimp_fwd_static", "linsimp_bwd", "linsimp_bwd_ex",
            "linsimp_prefill",
-           "linsimp_decode_step", "linsimp_decode_chunk", "linsimp_timing_enable",
+           "linsimp_decode_step", "linsimp_decode_chunk",
+           "linsimp_attn_workspace_size", "linsimp_attn_fwd", "linsimp_attn_bwd", "linsimp_attn_step",
+           "linsimp_timing_enable",
            "linsimp_timing_read", "linsimp_last_error", "linsimp_version")
 HEAD_EXPORTS = ("linsimp_head_saved_size", "linsimp_head_workspace_size", "linsimp_head_fwd",
                 "linsimp_head_bwd", "linsimp_head_bwd_ex")
@@ -82,6 +91,15 @@ def lib():
     L.linsimp_decode_step.restype = ctypes.c_int
     L.linsimp_decode_chunk.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32, f32] + [vp] * 13 + [vp]
     L.linsimp_decode_chunk.restype = ctypes.c_int
+    pa = ctypes.POINTER(AttnDims)
+    L.linsimp_attn_workspace_size.argtypes = [pa, ctypes.c_int]
+    L.linsimp_attn_workspace_size.restype = sz
+    L.linsimp_attn_fwd.argtypes = [pa] + [vp] * 7 + [vp, sz, vp]
+    L.linsimp_attn_fwd.restype = ctypes.c_int
+    L.linsimp_attn_bwd.argtypes = [pa] + [vp] * 11 + [vp, sz, vp]
+    L.linsimp_attn_bwd.restype = ctypes.c_int
+    L.linsimp_attn_step.argtypes = [pa] + [vp] * 7 + [vp, sz, vp]
+    L.linsimp_attn_step.restype = ctypes.c_int
     L.linsimp_timing_enable.argtypes = [ctypes.c_int]
     L.linsimp_timing_enable.restype = ctypes.c_int
     L.linsimp_timing_read.argtypes = [ctypes.c_char_p, ctypes.c_int, ctypes.POINTER(ctypes.c_float),
@@ -460,3 +478,109 @@ def feature_bank(gauss, radii, m, sign_correct=True, omega=None):
     _check(lib().linsimp_feature_bank(H, m, D, _ptr(gauss, "gauss"), _ptr(radii, "radii"),
                                       _ptr(omega, "omega"), 1 if sign_correct else 0, _stream()))
     return omega
+
+
+# ---------------------------------------------------------------------------
+# The mixers a LinSimp stack interleaves with (include/linsimp.h)
+# ---------------------------------------------------------------------------
+
+def alloc_bytes(nbytes: int, device) -> torch.Tensor:
+    """A 256-byte aligned workspace of ``nbytes`` bytes."""
+    return _aligned_bytes(nbytes, device)
+
+
+def attn_dims(q, k, causal=True, window=0, scale=None) -> AttnDims:
+    """Dims of an attention call from q [B, H, nq, D] and k [B, Hkv, nk, D]."""
+    if q.dim() != 4 or k.dim() != 4:
+        raise ValueError("q must be [B, H, nq, D] and k [B, Hkv, nk, D]")
+    B, H, nq, D = q.shape
+    return AttnDims(B, H, k.shape[1], nq, k.shape[2], window, D, _dtype_code(q), 1 if causal else 0,
+                    D ** -0.5 if scale is None else scale)
+
+
+def attn_workspace_size(d: AttnDims, backward: bool) -> int:
+    return int(lib().linsimp_attn_workspace_size(ctypes.byref(d), 1 if backward else 0))
+
+
+def _mixer_workspace(workspace, nbytes, device):
+    if nbytes == 0:
+        _check(-2)                                     # the message of the refused dims
+    if workspace is None:
+        return alloc_bytes(nbytes, device)
+    if workspace.get_device() != device.index:
+        raise ValueError(f"workspace is on {workspace.device}, expected {device}")
+    return workspace
+
+
+def _with_optional(pairs, optional):
+    """_expect over the required (tensor, name, shape, dtype) and those of
+    ``optional`` that are given; the addresses of both, None for the others."""
+    ptrs = _expect(pairs + [p for p in optional if p[0] is not None])
+    it = iter(ptrs[len(pairs):])
+    return ptrs[:len(pairs)], [next(it) if p[0] is not None else None for p in optional]
+
+
+def _attn_inputs(q, k, v, d):
+    return [(q, "q", (d.B, d.H, d.nq, d.D), q.dtype), (k, "k", (d.B, d.Hkv, d.nk, d.D), q.dtype),
+            (v, "v", (d.B, d.Hkv, d.nk, d.D), q.dtype)]
+
+
+def _attn_lens(lens_q, lens_k, B):
+    return [(lens_q, "lens_q", (B,), torch.int32), (lens_k, "lens_k", (B,), torch.int32)]
+
+
+def attn_fwd(q, k, v, causal=True, window=0, scale=None, lens_q=None, lens_k=None, out=None, lse=None,
+             want_lse=True, workspace=None):
+    """Softmax attention of q [B, H, nq, D] over k, v [B, Hkv, nk, D]; returns
+    (out, lse).  See linsimp_attn_fwd."""
+    d = attn_dims(q, k, causal, window, scale)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if lse is None and want_lse:
+        lse = torch.empty(q.shape[:3], dtype=torch.float32, device=q.device)
+    ptrs, (pq, pk, pl) = _with_optional(
+        _attn_inputs(q, k, v, d) + [(out, "out", q.shape, q.dtype)],
+        _attn_lens(lens_q, lens_k, d.B) + [(lse, "lse", q.shape[:3], torch.float32)])
+    workspace = _mixer_workspace(workspace, attn_workspace_size(d, False), q.device)
+    _check(lib().linsimp_attn_fwd(ctypes.byref(d), *ptrs[:3], pq, pk, ptrs[3], pl, _ptr(workspace, "workspace"),
+                                  workspace.numel(), _stream()))
+    return out, lse
+
+
+def attn_bwd(q, k, v, out, lse, dout, causal=True, window=0, scale=None, lens_q=None, lens_k=None, grads=None,
+             workspace=None):
+    """Backward of attn_fwd from what it returned; returns (dq, dk, dv).  See
+    linsimp_attn_bwd."""
+    d = attn_dims(q, k, causal, window, scale)
+    if grads is None:
+        grads = tuple(torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k, v))
+    ptrs, (pq, pk) = _with_optional(
+        _attn_inputs(q, k, v, d)
+        + [(out, "out", q.shape, q.dtype), (lse, "lse", q.shape[:3], torch.float32), (dout, "dout", q.shape, q.dtype)]
+        + [(g, "d" + nm, x.shape, x.dtype) for g, nm, x in zip(grads, "qkv", (q, k, v))],
+        _attn_lens(lens_q, lens_k, d.B))
+    workspace = _mixer_workspace(workspace, attn_workspace_size(d, True), q.device)
+    _check(lib().linsimp_attn_bwd(ctypes.byref(d), *ptrs[:3], pq, pk, *ptrs[3:], _ptr(workspace, "workspace"),
+                                  workspace.numel(), _stream()))
+    return tuple(grads)
+
+
+def attn_step(kcache, vcache, pos, q, k, v, scale=None, out=None, workspace=None):
+    """One decode step: token pos[b] (q [B, H, D], k, v [B, Hkv, D]) enters the ring
+    caches [B, Hkv, slots, D] in place; returns out [B, H, D].  See
+    linsimp_attn_step."""
+    if q.dim() != 3 or kcache.dim() != 4:
+        raise ValueError("q must be [B, H, D] and kcache [B, Hkv, slots, D]")
+    B, H, D = q.shape
+    Hkv, cap = kcache.shape[1], kcache.shape[2]
+    d = AttnDims(B, H, Hkv, 1, cap, 0, D, _dtype_code(q), 1, D ** -0.5 if scale is None else scale)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    dt = q.dtype
+    ptrs = _expect([(q, "q", (B, H, D), dt), (k, "k", (B, Hkv, D), dt), (v, "v", (B, Hkv, D), dt),
+                    (kcache, "kcache", (B, Hkv, cap, D), dt), (vcache, "vcache", (B, Hkv, cap, D), dt),
+                    (pos, "pos", (B,), torch.int64), (out, "out", (B, H, D), dt)])
+    workspace = _mixer_workspace(workspace, attn_workspace_size(d, False), q.device)
+    _check(lib().linsimp_attn_step(ctypes.byref(d), *ptrs, _ptr(workspace, "workspace"), workspace.numel(),
+                                   _stream()))
+    return out
