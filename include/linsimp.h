@@ -208,8 +208,8 @@ int linsimp_decode_chunk(int64_t S, int32_t H, int32_t T, int32_t D, int32_t Dv,
 
 /* ---- The mixers that a LinSimp stack interleaves with ----
  *
- * Softmax attention (the layers between the LinSimp layers of the paper's
- * Attn+LinSimp models, Sec. 4), behind the conventions
+ * Softmax attention and the gated linear recurrence (the layers between the
+ * LinSimp layers of the paper's hybrid models, Sec. 4), behind the conventions
  * above: dense [B, heads, rows, D] device tensors, 16-byte aligned, the
  * caller's workspace (256-byte aligned), calls that only enqueue on `stream`,
  * negative statuses.  D is 32, 64 or 128 with LINSIMP_BF16 and 32 or 64 with
@@ -274,6 +274,51 @@ int linsimp_attn_bwd(const linsimp_attn_dims* dims, const void* q, const void* k
 int linsimp_attn_step(const linsimp_attn_dims* dims, const void* q, const void* k, const void* v,
                       void* kcache, void* vcache, const int64_t* pos, void* out, void* workspace,
                       size_t workspace_bytes, void* stream);
+
+typedef struct {
+  int64_t B, H;    /* batch (sequences), heads                   */
+  int64_t n;       /* rows                                       */
+  int32_t D;       /* width of q, k, g, v, out                   */
+  int32_t dtype;   /* linsimp_dtype                              */
+  float scale;     /* on the output; finite                      */
+} linsimp_glr_dims;
+
+/* Bytes of workspace linsimp_glr_fwd (for_backward = 0) or linsimp_glr_bwd (1;
+ * enough for the forward too) needs.  0 for invalid or unsupported dims. */
+size_t linsimp_glr_workspace_size(const linsimp_glr_dims* dims, int for_backward);
+
+/* Gated linear recurrence (linear attention with a decay per key channel and
+ * row), forward:
+ *   S_t = diag(exp(g_t)) S_{t-1} + k_t v_t^T,   out_t = scale S_t^T q_t
+ *   q, k, v, g : [B, H, n, D] dtype;  out : [B, H, n, D] dtype, written
+ *   g    : logarithm of the decay, <= 0; -inf clears the channel
+ *   s0   : [B, H, D, D] float32 state before the first row (rows: key channel),
+ *          or NULL (zero);  s1 : the state after the last row, or NULL.  s1 may
+ *          be s0.
+ *   lens : [B] int32 on the device or NULL (n): rows of each sequence that
+ *          exist, values outside [0, n] taken as the nearest end.  Later rows
+ *          are not used, whatever they hold; their out is written as zeros and
+ *          s1 is the state after the last row that exists. */
+int linsimp_glr_fwd(const linsimp_glr_dims* dims, const void* q, const void* k, const void* v,
+                    const void* g, const float* s0, const int32_t* lens, void* out, float* s1,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* Backward: exact gradient of sum(dout * out) + sum(ds1 * s1); the states are
+ * recomputed.
+ *   q, k, v, g, s0, lens : as passed to the forward;  dout : [B, H, n, D] dtype
+ *   ds1 : [B, H, D, D] float32 gradient of the final state, or NULL (zero)
+ *   dq, dk, dv, dg : [B, H, n, D] dtype, overwritten (zeros in rows that do not
+ *         exist);  ds0 : [B, H, D, D] float32, or NULL. */
+int linsimp_glr_bwd(const linsimp_glr_dims* dims, const void* q, const void* k, const void* v,
+                    const void* g, const float* s0, const int32_t* lens, const void* dout,
+                    const float* ds1, void* dq, void* dk, void* dv, void* dg, float* ds0,
+                    void* workspace, size_t workspace_bytes, void* stream);
+
+/* One decode step for B sequences: state [B, H, D, D] float32 is updated in
+ * place with the token's k, g, v and read with its q.
+ *   q, k, v, g, out : [B, H, D] dtype;  dims->n must be 1.  Uses no workspace. */
+int linsimp_glr_step(const linsimp_glr_dims* dims, const void* q, const void* k, const void* v,
+                     const void* g, float* state, void* out, void* stream);
 
 /* Per-kernel timing, for tuning and roofline reports.  While enabled
  * (on != 0), every kernel the library launches is bracketed by two HIP events

@@ -22,7 +22,7 @@ LIBDIR = os.path.join(PKG, "_lib")
 LIB = os.path.join(LIBDIR, "liblinsimp.so")
 
 SOURCES = ["api.cpp", "fwd.hip", "prefill.hip", "bwd.hip", "decode.hip", "head.hip", "bank.hip",
-           "attn.hip", "mixers.cpp"]
+           "attn.hip", "glr.hip", "mixers.cpp"]
 ARCH = "gfx950"
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 

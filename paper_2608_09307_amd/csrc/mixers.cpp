@@ -1,10 +1,11 @@
-// C ABI of softmax attention: argument
+// C ABI of softmax attention and the gated linear recurrence: argument
 // validation, workspace carving and dispatch.  Contracts: include/linsimp.h.
 #include "../../include/linsimp.h"
 
 #include <math.h>
 
 #include "attn.h"
+#include "glr.h"
 #include "linsimp_internal.h"
 
 using namespace linsimp;
@@ -93,6 +94,51 @@ AttnArgs attn_args(const AttnShape& s) {
   return a;
 }
 
+int check_glr(const linsimp_glr_dims* d, GlrShape* s, bool step = false) {
+  if (d == nullptr) { set_error("dims is NULL"); return LINSIMP_E_INVALID_ARG; }
+  if (d->B < 1 || d->H < 1 || d->n < 1) {
+    set_error("glr: sizes must be positive (B=%lld H=%lld n=%lld)", (long long)d->B, (long long)d->H, (long long)d->n);
+    return LINSIMP_E_INVALID_ARG;
+  }
+  if (int rc = check_width("glr", d->D, d->dtype)) return rc;
+  if (!isfinite(d->scale)) { set_error("glr: scale must be finite"); return LINSIMP_E_INVALID_ARG; }
+  // (sequence, head) pairs index the scan's grid (the step's: a grid of fewer than 2^32 threads)
+  const int64_t big = (int64_t)1 << 30, most = step ? ((int64_t)1 << 24) - 1 : 65535;
+  if (d->B > big || d->H > big || d->n > big || d->B * d->H > most || d->B * d->H * d->n > (int64_t)1 << 31) {
+    set_error("glr: sizes too large: B*H at most %lld, n at most 2^30, B*H*n at most 2^31", (long long)most);
+    return LINSIMP_E_UNSUPPORTED;
+  }
+  s->B = d->B; s->H = d->H; s->n = d->n; s->D = d->D; s->dtype = d->dtype; s->scale = d->scale;
+  return LINSIMP_OK;
+}
+
+// which segments need the exact way; G > 1: their states and decays (backward: both directions); backward: the chunk states
+size_t glr_ws(const GlrShape& s, int G, bool backward, GlrArgs* a, void* base) {
+  const size_t BH = (size_t)s.BH(), DD = (size_t)s.D * s.D;
+  size_t off = 0;
+  auto take = [&](size_t bytes) {
+    void* p = base ? (char*)base + off : nullptr;
+    off += al(bytes);
+    return p;
+  };
+  int* again = (int*)take(BH * G * 4);
+  float* part = G > 1 ? (float*)take(BH * G * DD * 4) : nullptr;
+  float* fac = G > 1 ? (float*)take(BH * G * s.D * 4) : nullptr;
+  float* rpart = G > 1 && backward ? (float*)take(BH * G * DD * 4) : nullptr;
+  float* rfac = G > 1 && backward ? (float*)take(BH * G * s.D * 4) : nullptr;
+  void* states = backward ? take(BH * (size_t)s.nch() * DD * s.esize()) : nullptr;
+  if (a) { a->again = again; a->part = part; a->fac = fac; a->rpart = rpart; a->rfac = rfac; a->states = states; }
+  return off;
+}
+
+GlrArgs glr_args(const GlrShape& s, bool backward) {
+  GlrArgs a{};
+  a.H = (int)s.H; a.n = (int)s.n; a.nch = (int)s.nch();
+  a.G = glr_segments(s, backward); a.cps = (a.nch + a.G - 1) / a.G;
+  a.scale = s.scale;
+  return a;
+}
+
 }  // namespace
 
 extern "C" {
@@ -159,6 +205,63 @@ int linsimp_attn_step(const linsimp_attn_dims* dims, const void* q, const void* 
   a.q = q; a.k = kcache; a.v = vcache; a.knew = k; a.vnew = v; a.pos = pos; a.out = out; a.ns = ns;
   attn_ws(s, ns, false, &a, workspace);
   return launch_attn_fwd(s, a, (hipStream_t)stream);
+}
+
+size_t linsimp_glr_workspace_size(const linsimp_glr_dims* dims, int for_backward) {
+  GlrShape s;
+  if (check_glr(dims, &s) != LINSIMP_OK) return 0;
+  const size_t fwd = glr_ws(s, glr_segments(s, false), false, nullptr, nullptr);
+  const size_t bwd = for_backward ? glr_ws(s, glr_segments(s, true), true, nullptr, nullptr) : 0;
+  return fwd > bwd ? fwd : bwd;
+}
+
+int linsimp_glr_fwd(const linsimp_glr_dims* dims, const void* q, const void* k, const void* v,
+                    const void* g, const float* s0, const int32_t* lens, void* out, float* s1,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  GlrShape s;
+  int rc = check_glr(dims, &s);
+  if (rc) return rc;
+  const void* ps[] = {q, k, v, g, out};
+  if ((rc = check_ptrs("q,k,v,g,out", ps, 5))) return rc;
+  if ((rc = check_opt("s0", s0, 15)) || (rc = check_opt("lens", lens, 3)) || (rc = check_opt("s1", s1, 15))) return rc;
+  GlrArgs a = glr_args(s, false);
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, glr_ws(s, a.G, false, nullptr, nullptr)))) return rc;
+  a.q = q; a.k = k; a.v = v; a.g = g; a.s0 = s0; a.lens = lens; a.out = out; a.s1 = s1;
+  a.exact = s1 != nullptr;
+  glr_ws(s, a.G, false, &a, workspace);
+  return launch_glr_fwd(s, a, (hipStream_t)stream);
+}
+
+int linsimp_glr_bwd(const linsimp_glr_dims* dims, const void* q, const void* k, const void* v,
+                    const void* g, const float* s0, const int32_t* lens, const void* dout,
+                    const float* ds1, void* dq, void* dk, void* dv, void* dg, float* ds0,
+                    void* workspace, size_t workspace_bytes, void* stream) {
+  GlrShape s;
+  int rc = check_glr(dims, &s);
+  if (rc) return rc;
+  const void* ps[] = {q, k, v, g, dout, dq, dk, dv, dg};
+  if ((rc = check_ptrs("q,k,v,g,dout,dq,dk,dv,dg", ps, 9))) return rc;
+  if ((rc = check_opt("s0", s0, 15)) || (rc = check_opt("lens", lens, 3)) || (rc = check_opt("ds1", ds1, 15)) ||
+      (rc = check_opt("ds0", ds0, 15)))
+    return rc;
+  GlrArgs a = glr_args(s, true);
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, glr_ws(s, a.G, true, nullptr, nullptr)))) return rc;
+  a.q = q; a.k = k; a.v = v; a.g = g; a.s0 = s0; a.lens = lens; a.dout = dout; a.ds1 = ds1;
+  a.dq = dq; a.dk = dk; a.dv = dv; a.dg = dg; a.ds0 = ds0;
+  a.exact = ds0 != nullptr;
+  glr_ws(s, a.G, true, &a, workspace);
+  return launch_glr_bwd(s, a, (hipStream_t)stream);
+}
+
+int linsimp_glr_step(const linsimp_glr_dims* dims, const void* q, const void* k, const void* v,
+                     const void* g, float* state, void* out, void* stream) {
+  GlrShape s;
+  int rc = check_glr(dims, &s, true);
+  if (rc) return rc;
+  if (s.n != 1) { set_error("glr step: n must be 1"); return LINSIMP_E_INVALID_ARG; }
+  const void* ps[] = {q, k, v, g, state, out};
+  if ((rc = check_ptrs("q,k,v,g,state,out", ps, 6))) return rc;
+  return launch_glr_step(s, q, k, v, g, state, out, (hipStream_t)stream);
 }
 
 }  // extern "C"

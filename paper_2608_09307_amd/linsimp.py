@@ -41,6 +41,11 @@ class AttnDims(ctypes.Structure):
                 ("scale", ctypes.c_float)]
 
 
+class GlrDims(ctypes.Structure):
+    _fields_ = [("B", ctypes.c_int64), ("H", ctypes.c_int64), ("n", ctypes.c_int64),
+                ("D", ctypes.c_int32), ("dtype", ctypes.c_int32), ("scale", ctypes.c_float)]
+
+
 class HeadOpts(ctypes.Structure):
     _fields_ = [("norm_eps", ctypes.c_float), ("rms_eps", ctypes.c_float), ("gate", ctypes.c_int32)]
 
@@ -54,6 +59,7 @@ EXPORTS = ("linsimp_workspace_size", "linsimp_fwd", "linsimp_fwd_static", "linsi
            "linsimp_prefill",
            "linsimp_decode_step", "linsimp_decode_chunk",
            "linsimp_attn_workspace_size", "linsimp_attn_fwd", "linsimp_attn_bwd", "linsimp_attn_step",
+           "linsimp_glr_workspace_size", "linsimp_glr_fwd", "linsimp_glr_bwd", "linsimp_glr_step",
            "linsimp_timing_enable",
            "linsimp_timing_read", "linsimp_last_error", "linsimp_version")
 HEAD_EXPORTS = ("linsimp_head_saved_size", "linsimp_head_workspace_size", "linsimp_head_fwd",
@@ -91,7 +97,7 @@ def lib():
     L.linsimp_decode_step.restype = ctypes.c_int
     L.linsimp_decode_chunk.argtypes = [i64, i32, i32, i32, i32, i32, i32, i32, f32] + [vp] * 13 + [vp]
     L.linsimp_decode_chunk.restype = ctypes.c_int
-    pa = ctypes.POINTER(AttnDims)
+    pa, pg = ctypes.POINTER(AttnDims), ctypes.POINTER(GlrDims)
     L.linsimp_attn_workspace_size.argtypes = [pa, ctypes.c_int]
     L.linsimp_attn_workspace_size.restype = sz
     L.linsimp_attn_fwd.argtypes = [pa] + [vp] * 7 + [vp, sz, vp]
@@ -100,6 +106,14 @@ def lib():
     L.linsimp_attn_bwd.restype = ctypes.c_int
     L.linsimp_attn_step.argtypes = [pa] + [vp] * 7 + [vp, sz, vp]
     L.linsimp_attn_step.restype = ctypes.c_int
+    L.linsimp_glr_workspace_size.argtypes = [pg, ctypes.c_int]
+    L.linsimp_glr_workspace_size.restype = sz
+    L.linsimp_glr_fwd.argtypes = [pg] + [vp] * 8 + [vp, sz, vp]
+    L.linsimp_glr_fwd.restype = ctypes.c_int
+    L.linsimp_glr_bwd.argtypes = [pg] + [vp] * 13 + [vp, sz, vp]
+    L.linsimp_glr_bwd.restype = ctypes.c_int
+    L.linsimp_glr_step.argtypes = [pg] + [vp] * 6 + [vp]
+    L.linsimp_glr_step.restype = ctypes.c_int
     L.linsimp_timing_enable.argtypes = [ctypes.c_int]
     L.linsimp_timing_enable.restype = ctypes.c_int
     L.linsimp_timing_read.argtypes = [ctypes.c_char_p, ctypes.c_int, ctypes.POINTER(ctypes.c_float),
@@ -498,8 +512,20 @@ def attn_dims(q, k, causal=True, window=0, scale=None) -> AttnDims:
                     D ** -0.5 if scale is None else scale)
 
 
+def glr_dims(q, scale=None) -> GlrDims:
+    """Dims of a recurrence call from q [B, H, n, D] (or [B, H, D]: one row)."""
+    if q.dim() not in (3, 4):
+        raise ValueError("q must be [B, H, n, D] or [B, H, D]")
+    B, H, D = q.shape[0], q.shape[1], q.shape[-1]
+    return GlrDims(B, H, q.shape[2] if q.dim() == 4 else 1, D, _dtype_code(q), D ** -0.5 if scale is None else scale)
+
+
 def attn_workspace_size(d: AttnDims, backward: bool) -> int:
     return int(lib().linsimp_attn_workspace_size(ctypes.byref(d), 1 if backward else 0))
+
+
+def glr_workspace_size(d: GlrDims, backward: bool) -> int:
+    return int(lib().linsimp_glr_workspace_size(ctypes.byref(d), 1 if backward else 0))
 
 
 def _mixer_workspace(workspace, nbytes, device):
@@ -583,4 +609,66 @@ def attn_step(kcache, vcache, pos, q, k, v, scale=None, out=None, workspace=None
     workspace = _mixer_workspace(workspace, attn_workspace_size(d, False), q.device)
     _check(lib().linsimp_attn_step(ctypes.byref(d), *ptrs, _ptr(workspace, "workspace"), workspace.numel(),
                                    _stream()))
+    return out
+
+
+def _glr_inputs(q, k, v, g):
+    return [(x, nm, q.shape, q.dtype) for x, nm in ((q, "q"), (k, "k"), (v, "v"), (g, "g"))]
+
+
+def glr_fwd(q, k, v, g, s0=None, lens=None, scale=None, out=None, s1=None, want_state=True, workspace=None):
+    """Gated linear recurrence over q, k, v, g [B, H, n, D]; returns (out, s1), s1
+    the state [B, H, D, D] after the last row (None without ``want_state``).
+    See linsimp_glr_fwd."""
+    d = glr_dims(q, scale)
+    st = (d.B, d.H, d.D, d.D)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, H, n, D]")
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    if s1 is None and want_state:
+        s1 = torch.empty(st, dtype=torch.float32, device=q.device)
+    ptrs, (p0, pl, p1) = _with_optional(
+        _glr_inputs(q, k, v, g) + [(out, "out", q.shape, q.dtype)],
+        [(s0, "s0", st, torch.float32), (lens, "lens", (d.B,), torch.int32), (s1, "s1", st, torch.float32)])
+    workspace = _mixer_workspace(workspace, glr_workspace_size(d, False), q.device)
+    _check(lib().linsimp_glr_fwd(ctypes.byref(d), *ptrs[:4], p0, pl, ptrs[4], p1, _ptr(workspace, "workspace"),
+                                 workspace.numel(), _stream()))
+    return out, s1
+
+
+def glr_bwd(q, k, v, g, dout, s0=None, lens=None, ds1=None, scale=None, grads=None, want_ds0=None, workspace=None):
+    """Backward of glr_fwd; returns (dq, dk, dv, dg, ds0), ds0 None unless there is
+    an s0 (or ``want_ds0``).  See linsimp_glr_bwd."""
+    d = glr_dims(q, scale)
+    st = (d.B, d.H, d.D, d.D)
+    if q.dim() != 4:
+        raise ValueError("q must be [B, H, n, D]")
+    if grads is None:
+        grads = tuple(torch.empty_like(x, memory_format=torch.contiguous_format) for x in (q, k, v, g))
+    ds0 = None
+    if want_ds0 if want_ds0 is not None else s0 is not None:
+        ds0 = torch.empty(st, dtype=torch.float32, device=q.device)
+    ptrs, (p0, pl, p1, pd) = _with_optional(
+        _glr_inputs(q, k, v, g) + [(dout, "dout", q.shape, q.dtype)]
+        + [(x, "d" + nm, q.shape, q.dtype) for x, nm in zip(grads, "qkvg")],
+        [(s0, "s0", st, torch.float32), (lens, "lens", (d.B,), torch.int32), (ds1, "ds1", st, torch.float32),
+         (ds0, "ds0", st, torch.float32)])
+    workspace = _mixer_workspace(workspace, glr_workspace_size(d, True), q.device)
+    _check(lib().linsimp_glr_bwd(ctypes.byref(d), *ptrs[:4], p0, pl, ptrs[4], p1, *ptrs[5:], pd,
+                                 _ptr(workspace, "workspace"), workspace.numel(), _stream()))
+    return (*grads, ds0)
+
+
+def glr_step(state, q, k, v, g, scale=None, out=None):
+    """One decode step (q, k, v, g: [B, H, D]); updates ``state`` [B, H, D, D] in
+    place and returns out [B, H, D].  See linsimp_glr_step."""
+    if q.dim() != 3:
+        raise ValueError("q must be [B, H, D]")
+    d = glr_dims(q, scale)
+    if out is None:
+        out = torch.empty_like(q, memory_format=torch.contiguous_format)
+    ptrs = _expect(_glr_inputs(q, k, v, g) + [(state, "state", (d.B, d.H, d.D, d.D), torch.float32),
+                                             (out, "out", q.shape, q.dtype)])
+    _check(lib().linsimp_glr_step(ctypes.byref(d), *ptrs, _stream()))
     return out

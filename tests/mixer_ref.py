@@ -4,6 +4,10 @@ change.
 
 Bounds count worst cases.  With u the unit roundoff of the stored type (bf16
 2^-8, float32 2^-24) and e = 2^-24 for every float32 operation:
+  recurrence  a pair's weight is a product of scaled rows, each rounded to the operand
+              type (u), of a rounded pair weight or state (u) and of float32 decays (whose
+              errors, with those of the float32 sums, are counted 4 n + 200 times e);
+              float32 states of bf16 inputs are sums of two-term rows (u^2)
   attention   a score is off by (D + 4) e sum_d |q_d k_d| scale (the sum, the scale, the
               subtraction of the frame, whose own size adds e |s|), so p by the same
               amount relative (and 4 e for the exponential); p is rounded to the operand
@@ -90,6 +94,66 @@ def attention(q, k, v, dout=None, causal=True, window=0, scale=None, lens_q=None
     bv += 1.01 * u * dv.abs() + 1e-30
     got = {"out": (out, bo), "lse": (lse, bl)}
     return got if dout is None else {**got, "dq": (dq, bq), "dk": (dk, bk), "dv": (dv, bv)}
+
+
+def recurrence(q, k, v, g, dout=None, s0=None, ds1=None, lens=None, scale=None):
+    """Values and bounds of out, s1 and, with dout, dq, dk, dv, dg, ds0 (row by row)."""
+    u = unit(q.dtype)
+    us = u * u if q.dtype == torch.bfloat16 else u
+    q, k, v, g = (x.detach().cpu().double().clone() for x in (q, k, v, g))
+    B, H, n, D = q.shape
+    scale = D ** -0.5 if scale is None else scale
+    ln = [n if lens is None else min(max(int(lens[b]), 0), n) for b in range(B)]
+    do = None if dout is None else dout.detach().cpu().double().clone()
+    for b in range(B):
+        for x in (q, k, v, g) + (() if do is None else (do,)):
+            x[b, :, ln[b]:] = 0
+    slop = (4 * n + 200) * E32
+    a = torch.exp(g)
+    zero = torch.zeros(B, H, D, D, dtype=torch.float64)
+    S = zero.clone() if s0 is None else s0.detach().cpu().double()
+    A = S.abs()
+    o, oa, dq, qa = (torch.zeros(B, H, n, D, dtype=torch.float64) for _ in range(4))
+    before = []                                                # diag(a_t) |S|_{t-1} and diag(a_t) S_{t-1}
+    for t in range(n):
+        before.append((S * a[:, :, t, :, None], A * a[:, :, t, :, None]))
+        S = before[t][0] + k[:, :, t, :, None] * v[:, :, t, None]
+        A = before[t][1] + (k[:, :, t, :, None] * v[:, :, t, None]).abs()
+        o[:, :, t] = scale * (q[:, :, t, :, None] * S).sum(2)
+        oa[:, :, t] = abs(scale) * (q[:, :, t, :, None].abs() * A).sum(2)
+        if do is not None:
+            dq[:, :, t] = scale * (S * do[:, :, t, None]).sum(3)
+            qa[:, :, t] = abs(scale) * (A * do[:, :, t, None].abs()).sum(3)
+    for b in range(B):
+        dq[b, :, ln[b]:] = 0
+    tiny = 1e-30
+    got = {"out": (o, 1.01 * (u * o.abs() + (3 * u + slop) * oa) + tiny), "s1": (S, 1.01 * (us + slop) * A + tiny)}
+    if do is None:
+        return got
+    R = zero.clone() if ds1 is None else ds1.detach().cpu().double()
+    Ra = R.abs()
+    dk, ka, dv, va, dg, ga, ch = (torch.zeros(B, H, n, D, dtype=torch.float64) for _ in range(7))
+    tail = torch.zeros(B, H, D, dtype=torch.float64)
+    for t in range(n - 1, -1, -1):
+        if t % 32 == 31 or t == n - 1:
+            tail = (Ra * A if t == n - 1 else Ra * (before[t + 1][1] / a[:, :, t + 1, :, None].clamp_min(1e-300))).sum(3)
+        R = R + scale * q[:, :, t, :, None] * do[:, :, t, None]
+        Ra = Ra + abs(scale) * (q[:, :, t, :, None] * do[:, :, t, None]).abs()
+        dk[:, :, t], ka[:, :, t] = (R * v[:, :, t, None]).sum(3), (Ra * v[:, :, t, None].abs()).sum(3)
+        dv[:, :, t], va[:, :, t] = (R * k[:, :, t, :, None]).sum(2), (Ra * k[:, :, t, :, None].abs()).sum(2)
+        dg[:, :, t], ga[:, :, t] = (R * before[t][0]).sum(3), (Ra * before[t][1]).sum(3)
+        tail = tail + q[:, :, t].abs() * qa[:, :, t] + k[:, :, t].abs() * ka[:, :, t]
+        ch[:, :, t] = tail
+        R, Ra = R * a[:, :, t, :, None], Ra * a[:, :, t, :, None]
+    for b in range(B):
+        for x in (dk, dv, dg):
+            x[b, :, ln[b]:] = 0
+    return {**got, "dq": (dq, 1.01 * (u * dq.abs() + (3 * u + slop) * qa) + tiny),
+            "dk": (dk, 1.01 * (u * dk.abs() + (3 * u + slop) * ka) + tiny),
+            "dv": (dv, 1.01 * (u * dv.abs() + (3 * u + slop) * va) + tiny),
+            # pairs that do not span a row cancel there to the float32 sums' error
+            "dg": (dg, 1.01 * (u * dg.abs() + (5 * u + slop) * ga + slop * ch) + tiny),
+            "ds0": (R, 1.01 * (us + slop) * Ra + tiny)}
 
 
 def within(got, ref, name):
