@@ -774,23 +774,21 @@ LS_DEV float rows_from(float x) {
 // rounded factors on both sides, so nothing is left of it there; the pairs of a
 // row with itself are left out of c and added to dq and dk apart.
 // ---------------------------------------------------------------------------
-template <typename T, int D> struct GlrBwd {
+template <typename T, int D, bool LOW> struct GlrBwd {
   static constexpr int NW = D / 32, NT = 128 * NW;
-  static constexpr int ST = D + tr_pad<T, D>(), WST = GlrBase<T>::WST;
-  static constexpr int NLO = sizeof(T) == 2 ? 1 : 0;
+  static constexpr int ST = D + tr_pad<T, D>(), WST = GlrBase<T>::WST, EST = 36;
   static constexpr int MAT = 32 * ST;
-  static constexpr int ELEMS = (8 + 2 * NLO) * MAT + NW * 32 * WST;
-  static constexpr int EST = 36;
+  static constexpr int ELEMS = (LOW ? 10 : 8) * MAT + 2 * NW * 32 * WST;
 };
 
-template <typename T, int D, bool EXACT>
+template <typename T, int D, bool EXACT, bool LOW>
 __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void k_glr_bwd(GlrArgs a) {
   using F = MF<T>;
-  using C = GlrBwd<T, D>;
+  using C = GlrBwd<T, D, LOW>;
   constexpr int NW = C::NW, ST = C::ST, NKS = GlrBase<T>::NKS;
   __shared__ __align__(16) T smem[C::ELEMS];
   __shared__ __align__(16) float sfz[2][D], spend[2][D], slo[D], sall[D], sw[D];
-  __shared__ __align__(16) float se[NW][32 * C::EST];          // e_t of the key waves' rows
+  __shared__ __align__(16) float se[2][NW][32 * C::EST];       // e_t of the key waves' rows
   __shared__ int sslow[2][NW];
   const int tid = threadIdx.x, lane = tid & 63, wv = uniform(tid >> 6);
   int l = lane, col = l & 31, h = l >> 5;
@@ -800,8 +798,8 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
   auto sK = [&](int i) { return smem + (2 + i) * C::MAT; };
   auto sV = [&](int i) { return smem + (4 + i) * C::MAT; };
   auto sO = [&](int i) { return smem + (6 + i) * C::MAT; };
-  auto sL = [&](int i) { return smem + (8 + i * C::NLO) * C::MAT; };
-  T* sg = smem + (8 + 2 * C::NLO) * C::MAT + w * 32 * C::WST;
+  auto sL = [&](int i) { return smem + (LOW ? 8 + i : 0) * C::MAT; };
+  auto sG = [&](int i) { return smem + (LOW ? 10 : 8) * C::MAT + (i * NW + w) * 32 * C::WST; };
   if (EXACT && a.again[blockIdx.x] == 0) return;
   const int bh = blockIdx.x / a.G, seg = blockIdx.x % a.G;
   const int len = glr_len(a, bh), c0 = seg * a.cps, c1 = min(a.nch, c0 + a.cps);
@@ -843,36 +841,13 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
   if (keys) {
     const int me = 32 * w + chan_of(col);
     load_state_t<NW>(l, R, src ? src + (size_t)me * D : nullptr);
-    Row16<T> rq, rk, rg;
-    auto load = [&](int c) {
-      const size_t at = base + (size_t)32 * c * D;
-      const unsigned off = lane_off<T, D>(l, c, a.n);
-      rq.load(lane_ptr((const T*)a.q + at, off)); rk.load(lane_ptr((const T*)a.k + at, off));
-      rg.load(lane_ptr((const T*)a.g + at, off));
-    };
-    if (cl > c0) load(cl - 1);
 #pragma unroll 1
     for (int c = cl - 1; c >= c0; --c) {
       l = lane_in(lane, c); col = l & 31; h = l >> 5;
       const int i = c & 1, t = 32 * c + col;
-      const bool ok = t < len;
-      rq.keep(ok); rk.keep(ok); rg.keep(ok);
-      put_row(sg + col * C::WST + 16 * h, rg);
-      wave_lds_sync();
-      {
-        f32x16 E;
-        const bool fast = gate_chunk<T, true>(l, sg, E, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w);
-        put_decayed(l, sK(i) + 32 * w, sK(i), ST, rk, E, -1.0f, 1.0f, false);
-        float f[16];
-#pragma unroll
-        for (int v = 0; v < 16; ++v) f[v] = fast_exp2(E[v]);
-        put_lane(se[w] + col * C::EST + 16 * h, f);
-#pragma unroll
-        for (int v = 0; v < 16; ++v) f[v] *= a.scale;
-        put_scaled(l, sQ(i) + 32 * w, sL(i) + 32 * w, ST, rq, f, a.exact);
-        if (l == 0) sslow[i][w] = !fast;
-      }
-      // this chunk's rows again where they are needed, and the next chunk's
+      const bool whole = 32 * c + 32 <= len, ok = t < len;
+      T* sg = sG(i);
+      // this chunk's rows where they are needed
       auto rows_of = [&](Row16<T>& xq, Row16<T>& xk) {
         const size_t at = base + (size_t)32 * c * D;
         const unsigned off = lane_off<T, D>(l, c, a.n);
@@ -897,35 +872,42 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
       Tile<T> dPt, dP;
       float diag = 0.0f, through = 0.0f;
       f32x16 aq = zero16(), ak = zero16();
-      auto pairs = [&]() {
-        f32x16 pt = zero16(), p = zero16();
-#pragma unroll
-        for (int et = 0; et < NW; ++et)
-#pragma unroll
-          for (int sp = 0; sp < F::CSTEPS; ++sp) {
-            const typename F::frag vf = F::ldc(vrow, 32 * et, sp, h), of = F::ldc(orow, 32 * et, sp, h);
-            pt = F::mma(vf, of, pt);
-            p = F::mma(of, vf, p);
-          }
+      auto keep_pairs = [&](f32x16 pt, f32x16 p) {
 #pragma unroll
         for (int v = 0; v < 16; ++v) diag += crow(v, h) == col ? pt[v] : 0.0f;
+        diag = half_swap_add(diag);
+        if (!EXACT || !slow) {                           // the strictly earlier pairs
+          const int x = col - 4 * h;
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            pt[v] = crow(v, 0) < x ? pt[v] : 0.0f;
+            p[v] = crow(v, 0) > x ? p[v] : 0.0f;
+          }
+        }
         dPt.set(pt);
         dP.set(p);
       };
-      auto outside = [&](float zc) {
+      auto outside = [&](float zc, auto with_pairs) {
+        f32x16 pt = zero16(), p = zero16();
 #pragma unroll
         for (int et = 0; et < NW; ++et) {
           R[et] *= zc;
 #pragma unroll
           for (int sp = 0; sp < F::CSTEPS; ++sp) {
+            const typename F::frag vf = F::ldc(vrow, 32 * et, sp, h), of = F::ldc(orow, 32 * et, sp, h);
+            if constexpr (decltype(with_pairs)::value) {
+              pt = F::mma(vf, of, pt);
+              p = F::mma(of, vf, p);
+            }
             const typename F::frag r = F::cfrag(R[et], sp);
             through = dot_add(r, z[et][sp], through);
-            aq = F::mma(z[et][sp], F::ldc(orow, 32 * et, sp, h), aq);
-            ak = F::mma(r, F::ldc(vrow, 32 * et, sp, h), ak);
+            aq = F::mma(z[et][sp], of, aq);
+            ak = F::mma(r, vf, ak);
           }
           __builtin_amdgcn_sched_barrier(0);             // (one tile's operands in registers at a time)
         }
         through = half_swap_add(through);
+        if constexpr (decltype(with_pairs)::value) keep_pairs(pt, p);
       };
       // W into sw: what passes through the chunk, and the pairs that start in it and end after it
       auto put_w = [&]() {
@@ -939,37 +921,35 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
         if ((col & 1) == 0) sw[32 * w + 16 * h + (col >> 1)] += ends;
         wave_lds_sync();
       };
-      // dg from the row sums; dq and dk with the pairs of a row with itself
+      // dg from the row sums
       auto put_dg = [&](float (&x)[16]) {
         float W[16];
         get_vec(l, sw + 32 * w, W);
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
           x[v] = W[v] + rows_from(x[v]);
-          x[v] = ok ? x[v] : 0.0f;
+        }
+        if (!whole) {
+#pragma unroll
+          for (int v = 0; v < 16; ++v) x[v] = ok ? x[v] : 0.0f;
         }
         if (t < a.n) store_row(lane_ptr((T*)a.dg + base + (size_t)32 * c * D, lane_off<T, D>(l, c, a.n)), x);
       };
-      auto put_grad = [&](void* g, const Row16<T>& other, float (&x)[16]) {
-        const float dd = half_swap_add(diag) * a.scale;
+      auto put_grad = [&](void* g, float (&x)[16]) {
+        if (!whole) {
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = ok ? x[v] + dd * other.at(v) : 0.0f;
+          for (int v = 0; v < 16; ++v) x[v] = ok ? x[v] : 0.0f;
+        }
         if (t < a.n) store_row(lane_ptr((T*)g + base + (size_t)32 * c * D, lane_off<T, D>(l, c, a.n)), x);
       };
       if (!EXACT || !slow) {
-        pairs();
-        no_hoist();                                      // (the rows are read again: kept, they would push R out)
-        __builtin_amdgcn_sched_barrier(0);
-        outside(sfz[i][me]);
-        Row16<T> xq, xk;
+        outside(sfz[i][me], std::integral_constant<bool, true>{});
         put_w();
         __builtin_amdgcn_sched_barrier(0);
-        rows_of(xq, xk);
-        if (c > c0) load(c - 1);
 #pragma unroll
         for (int sp = 0; sp < F::CSTEPS; ++sp) {
-          aq = F::mma(rows_crow<true>(l, sK(i), ST, sp, 32 * w), dPt.keep(l, sp, [](int s, int t_) { return s < t_; }), aq);
-          ak = F::mma(rows_crow<true>(l, sQ(i), ST, sp, 32 * w), dP.keep(l, sp, [](int t_, int s) { return s < t_; }), ak);
+          aq = F::mma(rows_crow<true>(l, sK(i), ST, sp, 32 * w), dPt.f[sp], aq);
+          ak = F::mma(rows_crow<true>(l, sQ(i), ST, sp, 32 * w), dP.f[sp], ak);
         }
 #pragma unroll
         for (int ks = 0; ks < NKS; ++ks) {
@@ -978,21 +958,26 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
           for (int et = 0; et < NW; ++et) R[et] = F::mma(rows_nat<false>(l, sO(i), ST, ks, 32 * et), b, R[et]);
         }
         __builtin_amdgcn_sched_barrier(0);
+        // (the pairs of a row with itself: dP_tt k_t = e_t dP_tt (k_t / e_t), and alike)
         float x[16], y[16];
         get_row(qme, x);
         get_row(kme, y);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) x[v] = x[v] * aq[v] - y[v] * ak[v];
+        for (int v = 0; v < 16; ++v) {
+          const float z = x[v] * aq[v] - y[v] * ak[v];
+          aq[v] = __builtin_fmaf(diag, y[v], aq[v]);
+          ak[v] = __builtin_fmaf(diag, x[v], ak[v]);
+          x[v] = z;
+        }
         put_dg(x);
         __builtin_amdgcn_sched_barrier(0);
-        get_lane(se[w] + col * C::EST + 16 * h, y);
+        get_lane(se[i][w] + col * C::EST + 16 * h, y);
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[v] = y[v] * a.scale * aq[v];
-        put_grad(a.dq, xk, x);
-        __builtin_amdgcn_sched_barrier(0);
+        put_grad(a.dq, x);
 #pragma unroll
         for (int v = 0; v < 16; ++v) x[v] = __builtin_amdgcn_rcpf(y[v]) * ak[v];
-        put_grad(a.dk, xq, x);
+        put_grad(a.dk, x);
       } else {
         // the exact way: what comes from outside the chunk last, so that the rows are scaled for it then
         float dq[16], dk[16], x[16];
@@ -1000,7 +985,7 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
         rows_of(xq, xk);
         xq.keep(ok); xk.keep(ok);
         gate_exact(l, sg);
-        pairs();
+        keep_pairs(rows_by_rows<T, NW>(h, vrow, orow), rows_by_rows<T, NW>(h, orow, vrow));
 #pragma unroll
         for (int v = 0; v < 16; ++v) dq[v] = dk[v] = x[v] = 0.0f;
 #pragma unroll 1
@@ -1032,14 +1017,14 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
           f32x16 B = gate_sum(l, sg, UpTo{});
 #pragma unroll
           for (int v = 0; v < 16; ++v) f[v] = ex(B[v]) * a.scale;
-          put_scaled(l, sQ(i) + 32 * w, sL(i) + 32 * w, ST, xq.again(), f, a.exact);
+          put_scaled(l, sQ(i) + 32 * w, sL(i) + 32 * w, ST, xq.again(), f, LOW);
           B = gate_sum(l, sg, After{});
 #pragma unroll
           for (int v = 0; v < 16; ++v) f[v] = ex(B[v]);
           put_scaled(l, sK(i) + 32 * w, sK(i), ST, xk.again(), f, false);
           __syncthreads();
         }
-        outside(sfz[i][me]);
+        outside(sfz[i][me], std::integral_constant<bool, false>{});
         through *= sall[me];
         put_w();
         float y[16];
@@ -1052,9 +1037,15 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 #pragma unroll
         for (int v = 0; v < 16; ++v) { x[v] -= y[v] * ak[v]; dk[v] += ex(B[v]) * ak[v]; }
         put_dg(x);
-        put_grad(a.dq, xk.again(), dq);
-        put_grad(a.dk, xq.again(), dk);
-        if (c > c0) load(c - 1);
+        const Row16<T> yq = xq.again(), yk = xk.again();
+        diag *= a.scale;
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          dq[v] = __builtin_fmaf(diag, yk.at(v), dq[v]);
+          dk[v] = __builtin_fmaf(diag, yq.at(v), dk[v]);
+        }
+        put_grad(a.dq, dq);
+        put_grad(a.dk, dk);
 #pragma unroll
         for (int et = 0; et < NW; ++et) R[et] *= sall[me];
 #pragma unroll
@@ -1067,22 +1058,45 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
     }
   } else {
     load_state<NW>(l, R, src, D, 32 * w + chan_of(col));
-    Row16<T> rv, ro;
+    // They also scale the key rows: while the key waves work on chunk c, chunk c - 1
+    // is staged, from rows loaded a chunk earlier.
+    Row16<T> rq, rk, rg, rv, ro;
     auto load = [&](int c) {
       const size_t at = base + (size_t)32 * c * D;
       const unsigned off = lane_off<T, D>(l, c, a.n);
-      rv.load(lane_ptr((const T*)a.v + at, off)); ro.load(lane_ptr((const T*)a.dout + at, off));
+      rg.load(lane_ptr((const T*)a.g + at, off)); rq.load(lane_ptr((const T*)a.q + at, off));
+      rk.load(lane_ptr((const T*)a.k + at, off)); rv.load(lane_ptr((const T*)a.v + at, off));
+      ro.load(lane_ptr((const T*)a.dout + at, off));
     };
-    if (cl > c0) load(cl - 1);
+    auto stage = [&](int c) {
+      const int i = c & 1;
+      const bool ok = 32 * c + col < len;
+      rq.keep(ok); rk.keep(ok); rg.keep(ok); rv.keep(ok); ro.keep(ok);
+      put_row(sG(i) + col * C::WST + 16 * h, rg);
+      put_row(sV(i) + col * ST + 32 * w + 16 * h, rv);
+      put_row(sO(i) + col * ST + 32 * w + 16 * h, ro);
+      wave_lds_sync();
+      f32x16 E;
+      const bool fast = gate_chunk<T, true>(l, sG(i), E, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w);
+      put_decayed(l, sK(i) + 32 * w, sK(i), ST, rk, E, -1.0f, 1.0f, false);
+      float f[16];
+#pragma unroll
+      for (int v = 0; v < 16; ++v) f[v] = fast_exp2(E[v]);
+      put_lane(se[i][w] + col * C::EST + 16 * h, f);
+#pragma unroll
+      for (int v = 0; v < 16; ++v) f[v] *= a.scale;
+      put_scaled(l, sQ(i) + 32 * w, sL(i) + 32 * w, ST, rq, f, LOW);
+      if (l == 0) sslow[i][w] = !fast;
+      if (c > c0) load(c - 1);
+    };
+    if (cl > c0) {
+      load(cl - 1);
+      stage(cl - 1);
+    }
 #pragma unroll 1
     for (int c = cl - 1; c >= c0; --c) {
       l = lane_in(lane, c); col = l & 31; h = l >> 5;
       const int i = c & 1, t = 32 * c + col;
-      const bool ok = t < len;
-      rv.keep(ok); ro.keep(ok);
-      put_row(sV(i) + col * ST + 32 * w + 16 * h, rv);
-      put_row(sO(i) + col * ST + 32 * w + 16 * h, ro);
-      if (c > c0) load(c - 1);
       __syncthreads();
       const bool slow = any_slow(i);
       if (!EXACT && slow) {
@@ -1128,15 +1142,16 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
         const typename F::frag b = rows_nat<true>(l, sO(i), ST, ks, 32 * w);
 #pragma unroll
         for (int dt = 0; dt < NW; ++dt) R[dt] = F::mma(rows_nat<false>(l, sQ(i), ST, ks, 32 * dt), b, R[dt]);
-        if (C::NLO && a.exact) {
+        if constexpr (LOW) {
 #pragma unroll
           for (int dt = 0; dt < NW; ++dt) R[dt] = F::mma(rows_nat<false>(l, sL(i), ST, ks, 32 * dt), b, R[dt]);
         }
       }
       float y[16];
 #pragma unroll
-      for (int v = 0; v < 16; ++v) y[v] = ok ? A[v] : 0.0f;
+      for (int v = 0; v < 16; ++v) y[v] = t < len ? A[v] : 0.0f;
       if (t < a.n) store_row(lane_ptr((T*)a.dv + base + (size_t)32 * c * D, lane_off<T, D>(l, c, a.n)), y);
+      if (c > c0) stage(c - 1);
     }
   }
   if (!EXACT && tid == 0) a.again[blockIdx.x] = gave_up;
@@ -1258,8 +1273,14 @@ template <typename T, int D> static int run_bwd(const GlrShape& s, const GlrArgs
   }
   if (int rc = launch_status("glr states")) return rc;
   ProfScope ps("glr_bwd", st);
-  k_glr_bwd<T, D, false><<<(unsigned)(s.BH() * a.G), 4 * D, 0, st>>>(a);
-  k_glr_bwd<T, D, true><<<(unsigned)(s.BH() * a.G), 4 * D, 0, st>>>(a);
+  const unsigned grid = (unsigned)(s.BH() * a.G);
+  if (sizeof(T) == 2 && a.exact) {
+    k_glr_bwd<T, D, false, sizeof(T) == 2><<<grid, 4 * D, 0, st>>>(a);
+    k_glr_bwd<T, D, true, sizeof(T) == 2><<<grid, 4 * D, 0, st>>>(a);
+  } else {
+    k_glr_bwd<T, D, false, false><<<grid, 4 * D, 0, st>>>(a);
+    k_glr_bwd<T, D, true, false><<<grid, 4 * D, 0, st>>>(a);
+  }
   return launch_status("glr backward");
 }
 
