@@ -13,12 +13,16 @@
 // operand type there (bf16: 2^-9 relative, random over the keys they are summed
 // over); scores, maxima, sums and outputs are float32 until the final store.
 #include "attn.h"
+
+#include <math.h>
+
 #include "common.h"
 #include "linsimp_internal.h"
 #include "prof.h"
 
 namespace linsimp {
 
+static constexpr int kMaxSplits = 64;
 static constexpr float kLn2 = 0.6931471805599453f;
 
 // A sequence's lengths and its mask: query i (position i + off) sees key j when
@@ -40,17 +44,18 @@ LS_DEV Seq seq_of(const AttnArgs& a, int b) {
   return s;
 }
 
-// Workgroup -> (tile, head).  Workgroups are dealt to the eight XCDs in turn;
-// with a multiple of eight heads each XCD walks whole heads, so that the tiles
-// which read the same keys share its L2.  Late tiles first: under a causal mask
-// they are the long ones (the key sweep's long ones are the early tiles).
+// Workgroup -> (tile, head).  Workgroups are dealt to the eight XCDs in turn, so
+// with a multiple of eight heads every XCD keeps whole heads, whose tiles share
+// its L2; the longest tiles of all of them come first (48 heads of 2048 tokens,
+// D = 64: key sweep 139 -> 105 us against whole heads in turn, which left a CU
+// with the long tiles of each).
 LS_DEV void tile_and_head(int nt, int heads, bool late_first, int& tile, int& head) {
   const int lin = (int)blockIdx.x;
   int t;
   if (heads % 8 == 0) {
-    const int slot = lin >> 3;
-    head = (lin & 7) + 8 * (slot / nt);
-    t = slot % nt;
+    const int hx = heads >> 3, slot = lin >> 3;
+    head = (lin & 7) + 8 * (slot % hx);
+    t = slot / hx;
   } else {
     head = lin % heads;
     t = lin / heads;
@@ -256,25 +261,40 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (a.lse != nullptr && h == 0) a.lse[row] = none ? kNegInf : (st.m + __log2f(lt)) * kLn2;
 }
 
-// Joins the ns partial results of every query row: D / 4 threads per row.
-template <typename T, int D>
+// Joins the ns partial results of query rows, one row at a time in each group of
+// D / 4 x P threads: P of them share the partial results of four columns.
+template <typename T, int D, int P>
 __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
-  constexpr int TPR = D / 4;
+  constexpr int TPR = D / 4, RPB = 256 / (TPR * P);       // threads across a row, rows per workgroup
+  __shared__ float sml[RPB][2 * kMaxSplits];
+  __shared__ __align__(16) float so[RPB][P][D + 4];
   const size_t rows = (size_t)a.B * a.H * a.nq;
-  const size_t row = (size_t)blockIdx.x * (256 / TPR) + threadIdx.x / TPR;
-  const int e0 = (threadIdx.x % TPR) * 4;
-  if (row >= rows) return;
+  const int tid = threadIdx.x, g = tid / (TPR * P), in = tid % (TPR * P), pr = in / TPR, e0 = (in % TPR) * 4;
+  const size_t row = (size_t)blockIdx.x * RPB + g;
+  const bool ok = row < rows;
+  for (int s = in; ok && s < a.ns; s += TPR * P)
+    *(float2*)&sml[g][2 * s] = *(const float2*)(a.pml + ((size_t)s * rows + row) * 2);
+  __syncthreads();
   float m = kNegInf;
-  for (int s = 0; s < a.ns; ++s) m = fmaxf(m, a.pml[((size_t)s * rows + row) * 2]);
+  for (int s = 0; ok && s < a.ns; ++s) m = fmaxf(m, sml[g][2 * s]);
   float l = 0.0f;
   f32x4 o = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll 4
-  for (int s = 0; s < a.ns; ++s) {
-    const float2 ml = *(const float2*)(a.pml + ((size_t)s * rows + row) * 2);
-    const float f = ml.x == kNegInf ? 0.0f : fast_exp2(ml.x - m);
-    const f32x4 x = *(const f32x4*)(a.part + ((size_t)s * rows + row) * D + e0);
-    l += ml.y * f;
-    o += x * f;
+  for (int s = pr; ok && s < a.ns; s += P) {
+    const float ms = sml[g][2 * s];
+    const float f = ms == kNegInf ? 0.0f : fast_exp2(ms - m);
+    o += *(const f32x4*)(a.part + ((size_t)s * rows + row) * D + e0) * f;
+    l += sml[g][2 * s + 1] * f;
+  }
+  *(f32x4*)(so[g][pr] + e0) = o;
+  if (e0 == 0) so[g][pr][D] = l;
+  __syncthreads();
+  if (!ok || pr != 0) return;
+  l = so[g][0][D];
+#pragma unroll
+  for (int p = 1; p < P; ++p) {
+    o += *(const f32x4*)(so[g][p] + e0);
+    l += so[g][p][D];
   }
   const int b = (int)(row / ((size_t)a.H * a.nq)), i = (int)(row % a.nq);
   const bool none = i >= (a.lens_q ? a.lens_q[b] : a.nq) || l == 0.0f;
@@ -722,26 +742,40 @@ static int launch_status(const char* what) {
 
 bool attn_few(const AttnShape& s) { return s.H / s.Hkv * s.nq <= 32; }
 
-// Workgroups that share one query tile's (or key head's) keys.  Time in units of
-// one key tile's work, `slots` workgroups running at once: rounds of workgroups
-// times (key tiles per split + the prologue and stores, about kEnds tiles), and
-// for more than one split the joining launch.
+// Workgroups that share one query tile's (or key head's) keys, from the time in
+// microseconds: the longest workgroup's key tiles and the whole load at the rate
+// of a full chip, which add up in squares (neither is hidden behind the other
+// when they are equal), and for more than one split the joining launch and the
+// partial results.  The constants are measured: a tile of 64 keys takes
+// 0.45 + 0.0075 D (float32: 0.3 + 0.05 D) on a CU, however many workgroups share
+// the CU; a round of 128 keys of the few-row kernel 0.9 + 0.005 D, and all of
+// them together the bytes of k and v at 5 TB/s.  E.g. 16 heads of 2048 tokens,
+// D = 128: 54 us in one piece, 46 in two; 4 heads' 64k keys for 16 heads and one
+// token: 800 us in one piece, 40 in 32 to 64.
 int attn_splits(const AttnShape& s) {
   const bool few = attn_few(s);
-  const int64_t groups = few ? s.B * s.Hkv : s.B * s.H * ((s.nq + 127) / 128);
-  int64_t span = s.nk;                                    // keys a workgroup walks
-  if (s.window > 0) span = span < s.window + 128 ? span : s.window + 128;
-  const int64_t tiles = few ? (span + 127) / 128 : (span + 63) / 64;
-  const double kEnds = few ? 1.0 : 3.0, kJoin = few ? 3.0 : 6.0;
-  const int64_t slots = 512;
-  if (groups >= 2 * slots) return 1;
+  const int64_t ntq = few ? 1 : (s.nq + 127) / 128;
+  const double groups = (double)(few ? s.B * s.Hkv * ((s.H / s.Hkv * s.nq + 31) / 32) : s.B * s.H * ntq);
+  double most = (double)s.nk, mean = (double)s.nk;        // keys of the longest and of the average workgroup
+  if (s.causal && !few && s.nq <= s.nk) mean = (double)s.nk - 0.5 * (double)s.nq;
+  if (s.window > 0) {
+    const double w = (double)(s.window + 128);
+    most = most < w ? most : w;
+    mean = mean < w ? mean : w;
+  }
+  const double tile = few ? 128.0 : 64.0;
+  const double us = few ? 0.9 + 0.005 * s.D : s.dtype == 1 ? 0.45 + 0.0075 * s.D : 0.3 + 0.05 * s.D;
+  const double bytes = 2.0 * s.D * (double)s.esize();     // of one key and value
+  const double partial = (double)(s.B * s.H * s.nq) * (s.D + 2) * 4.0;
   int best = 1;
   double best_t = 1e300;
-  for (int64_t n = 1; n <= 64 && n <= tiles; ++n) {
-    const double rounds = (double)((groups * n + slots - 1) / slots);
-    double t = rounds * ((double)((tiles + n - 1) / n) + kEnds);
-    if (n > 1) t += kJoin + 0.02 * n;
-    if (t < best_t) { best_t = t; best = (int)n; }
+  for (int n = 1; n <= kMaxSplits && (n == 1 || n * tile < most + tile); ++n) {
+    const double longest = (most / tile / n + (few ? 1.5 : 3.0)) * us;
+    const double load = few ? groups * mean * bytes / 5e6 + groups * n * 2.0 * us / 512
+                            : groups * n * (mean / tile / n + 3.0) * us * 0.9 / 256;
+    double t = sqrt(longest * longest + load * load);
+    if (n > 1) t += 4.0 + n * partial / 4e6;
+    if (t < 0.98 * best_t) { best_t = t; best = n; }
   }
   return best;
 }
@@ -761,9 +795,11 @@ static int run_fwd(const AttnShape& s, AttnArgs a, hipStream_t st) {
   }
   if (int rc = launch_status(what)) return rc;
   if (a.ns > 1) {
-    const int64_t rows = s.B * s.H * s.nq, per = 256 / (D / 4);
+    // many rows: one set of threads per row; few: all of a workgroup on one
+    const int64_t rows = s.B * s.H * s.nq;
     ProfScope ps("attn_join", st);
-    k_attn_join<T, D><<<(unsigned)((rows + per - 1) / per), 256, 0, st>>>(a);
+    if (rows >= 4096) k_attn_join<T, D, 1><<<(unsigned)((rows + 1024 / D - 1) / (1024 / D)), 256, 0, st>>>(a);
+    else k_attn_join<T, D, 1024 / D><<<(unsigned)rows, 256, 0, st>>>(a);
     return launch_status("attn join");
   }
   return 0;
