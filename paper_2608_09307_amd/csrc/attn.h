@@ -23,14 +23,16 @@ struct AttnArgs {
   float* lse;                    // [B][H][nq] natural logarithm, or null
   const void* dout;
   void *dq, *dk, *dv;
-  float *part, *pml;             // ns > 1: [ns][B][H][nq][D] unnormalised outputs, [..][2] maximum (log2) and sum
+  float *part, *pml;             // ns > 1: [ns][B][H][nq][D] unnormalised outputs, [..][2] maximum (log2) and sum;
+                                 // backward, nsq or nsk > 1: the splits' gradients (dq's, then dk's and dv's)
   float* delta;                  // [B][H][nq]
   int B, H, Hkv, G, nq, nk, causal, window;
-  int ntq, ntk, ns;              // query and key tiles of 128, key splits
+  int ntq, ntk, ns, nsq, nsk;    // query and key tiles of 128; splits of the forward, the query and the key sweep
   float scale, c;                // c = scale log2(e)
 };
 
 int attn_splits(const AttnShape& s);
+void attn_bwd_splits(const AttnShape& s, int* nsq, int* nsk);
 int launch_attn_fwd(const AttnShape& s, const AttnArgs& a, hipStream_t st);
 int launch_attn_bwd(const AttnShape& s, const AttnArgs& a, hipStream_t st);
 

@@ -63,6 +63,24 @@ LS_DEV void tile_and_head(int nt, int heads, bool late_first, int& tile, int& he
   tile = late_first ? nt - 1 - t : t;
 }
 
+// Staging of row tiles (common.h) with one address for the workgroup and an offset
+// in 32 bits per lane: rows row0 .. of a dense [*, COLS] matrix of `rows` rows,
+// those past its end read from its last one (and staged as zeros).
+template <typename T, int ROWS, int COLS, int NT>
+struct TileRows : StageRows<T, ROWS, COLS, NT> {
+  using S = StageRows<T, ROWS, COLS, NT>;
+  LS_DEV void load(const T* g, int row0, int rows, int tid) {
+    const int at = min(row0, rows - 1), last = rows - 1 - at;
+    const char* base = (const char*)(g + (size_t)at * COLS);
+#pragma unroll
+    for (int it = 0; it < S::IT; ++it) {
+      const int idx = min(tid + NT * it, S::N - 1);
+      const unsigned off = (unsigned)((min(idx / S::CPR, last) * COLS + (idx % S::CPR) * S::VE) * (int)sizeof(T));
+      this->x[it] = *(const typename S::V*)(base + off);
+    }
+  }
+};
+
 // operand fragments of one row of a dense [*, D] matrix (lane's row, its half's k)
 template <typename T, int D>
 LS_DEV void row_frags(typename MF<T>::frag (&f)[D / MF<T>::KS], const T* row) {
@@ -191,14 +209,14 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   row_frags<T, D>(qf, (const T*)a.q + ((size_t)bh * a.nq + min(qi, a.nq - 1)) * D);
   Online<D> st;
   st.clear();
-  StageRows<T, KT, D, C::NT> rk, rv;
+  TileRows<T, KT, D, C::NT> rk, rv;
   if (t0 < t1) {
-    rk.load(ks, D, t0 * KT, 0, sq.lk, tid);
-    rv.load(vs, D, t0 * KT, 0, sq.lk, tid);
+    rk.load(ks, t0 * KT, sq.lk, tid);
+    rv.load(vs, t0 * KT, sq.lk, tid);
     rk.store(sK(0), C::KST, t0 * KT, 0, sq.lk, tid);
     rv.store(sV(0), C::VST, t0 * KT, 0, sq.lk, tid);
-    rk.load(ks, D, (t0 + 1) * KT, 0, sq.lk, tid);
-    rv.load(vs, D, (t0 + 1) * KT, 0, sq.lk, tid);
+    rk.load(ks, (t0 + 1) * KT, sq.lk, tid);
+    rv.load(vs, (t0 + 1) * KT, sq.lk, tid);
   }
   const int wlo = sq.lo(qw), whi = sq.hi(min(qw + 31, sq.lq - 1));      // keys any of the wave's queries sees
   const int alo = sq.lo(qw + 31), ahi = sq.hi(qw);                      // keys all of them see
@@ -209,8 +227,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     if (t + 1 < t1) {
       rk.store(sK(cur ^ 1), C::KST, k0 + KT, 0, sq.lk, tid);
       rv.store(sV(cur ^ 1), C::VST, k0 + KT, 0, sq.lk, tid);
-      rk.load(ks, D, k0 + 2 * KT, 0, sq.lk, tid);
-      rv.load(vs, D, k0 + 2 * KT, 0, sq.lk, tid);
+      rk.load(ks, k0 + 2 * KT, sq.lk, tid);
+      rv.load(vs, k0 + 2 * KT, sq.lk, tid);
     }
     if (qw >= sq.lq || k0 > whi || k0 + KT <= wlo) continue;
     f32x16 s[KT / 32];
@@ -501,8 +519,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   auto sK = [&](int i) { return smem + i * C::KB; };
   auto sV = [&](int i) { return smem + 2 * C::KB + i * C::VB; };
   const int tid = threadIdx.x, l = tid & 63, col = l & 31, h = l >> 5, wv = uniform(tid >> 6);
-  int tile, bh;
-  tile_and_head(a.ntq, a.B * a.H, a.causal, tile, bh);
+  int tile, bhs;
+  tile_and_head(a.ntq, a.B * a.H * a.nsq, a.causal, tile, bhs);
+  const int bh = bhs / a.nsq, sp = bhs % a.nsq;
   const int b = bh / a.H, kh = (bh % a.H) / a.G;
   const Seq sq = seq_of(a, b);
   const int q0 = tile * C::BQ, qw = q0 + wv * 32, qi = qw + col;
@@ -511,8 +530,10 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   int t0 = 0, t1 = 0;
   if (q0 < sq.lq) {
     const int qe = min(q0 + C::BQ, sq.lq) - 1;
-    t0 = sq.lo(q0) / KT;
-    t1 = sq.hi(qe) < 0 ? 0 : sq.hi(qe) / KT + 1;
+    const int first = sq.lo(q0) / KT, last = sq.hi(qe) < 0 ? -1 : sq.hi(qe) / KT;
+    const int per = (last - first + a.nsq) / a.nsq;
+    t0 = first + sp * per;
+    t1 = min(last + 1, t0 + per);
   }
   const size_t row = (size_t)bh * a.nq + min(qi, a.nq - 1);
   typename F::frag qf[D / F::KS], of[D / F::KS];
@@ -533,19 +554,19 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   // the products start from -lse / scale (-inf: a row without keys) and -delta
   const float s0 = live ? -a.lse[row] * kLog2e / a.c : kNegInf;
   if (!live) delta = 0.0f;
-  if (qi < a.nq && h == 0) a.delta[row] = delta;
+  if (qi < a.nq && h == 0 && sp == 0) a.delta[row] = delta;
 
   f32x16 acc[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) acc[dt] = zero16();
-  StageRows<T, KT, D, C::NT> rk, rv;
+  TileRows<T, KT, D, C::NT> rk, rv;
   if (t0 < t1) {
-    rk.load(ks, D, t0 * KT, 0, sq.lk, tid);
-    rv.load(vs, D, t0 * KT, 0, sq.lk, tid);
+    rk.load(ks, t0 * KT, sq.lk, tid);
+    rv.load(vs, t0 * KT, sq.lk, tid);
     rk.store(sK(0), C::KST, t0 * KT, 0, sq.lk, tid);
     rv.store(sV(0), C::VST, t0 * KT, 0, sq.lk, tid);
-    rk.load(ks, D, (t0 + 1) * KT, 0, sq.lk, tid);
-    rv.load(vs, D, (t0 + 1) * KT, 0, sq.lk, tid);
+    rk.load(ks, (t0 + 1) * KT, sq.lk, tid);
+    rv.load(vs, (t0 + 1) * KT, sq.lk, tid);
   }
   const int wlo = sq.lo(qw), whi = sq.hi(min(qw + 31, sq.lq - 1));
   const int alo = sq.lo(qw + 31), ahi = qw + 31 < sq.lq ? sq.hi(qw) : -1;
@@ -556,8 +577,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     if (t + 1 < t1) {
       rk.store(sK(cur ^ 1), C::KST, k0 + KT, 0, sq.lk, tid);
       rv.store(sV(cur ^ 1), C::VST, k0 + KT, 0, sq.lk, tid);
-      rk.load(ks, D, k0 + 2 * KT, 0, sq.lk, tid);
-      rv.load(vs, D, k0 + 2 * KT, 0, sq.lk, tid);
+      rk.load(ks, k0 + 2 * KT, sq.lk, tid);
+      rv.load(vs, k0 + 2 * KT, sq.lk, tid);
     }
     if (qw >= sq.lq || k0 > whi || k0 + KT <= wlo) continue;
     const T* krow = sK(cur) + col * C::KST;
@@ -588,7 +609,27 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         acc[dt] = F::mma(F::tld_crow(sK(cur), C::KST, 0, i, dt * 32), p, acc[dt]);
     }
   }
-  if (qi < a.nq) store_col<T, D>((T*)a.dq + row * D, acc, a.scale);
+  if (qi >= a.nq) return;
+  if (a.nsq > 1) store_col<float, D>(a.part + ((size_t)sp * a.B * a.H * a.nq + row) * D, acc, a.scale);
+  else store_col<T, D>((T*)a.dq + row * D, acc, a.scale);
+}
+
+// The gradients of split sweeps: the ns partial sums of n elements, in order
+// (blockIdx.y: of the first and of the second result).
+template <typename T>
+__global__ __launch_bounds__(256) void k_attn_sum(const float* part, T* out0, T* out1, size_t n, int ns) {
+  typedef T V4 __attribute__((ext_vector_type(4)));
+  const size_t i = ((size_t)blockIdx.x * 256 + threadIdx.x) * 4;
+  T* out = blockIdx.y ? out1 : out0;
+  part += (size_t)blockIdx.y * ns * n;
+  if (i >= n) return;
+  f32x4 x = {0.f, 0.f, 0.f, 0.f};
+#pragma unroll 8
+  for (int s = 0; s < ns; ++s) x += *(const f32x4*)(part + (size_t)s * n + i);
+  V4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (T)x[e];
+  *(V4*)(out + i) = y;
 }
 
 // ---------------------------------------------------------------------------
@@ -618,20 +659,21 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   auto sQ = [&](int i) { return smem + i * C::QB; };
   auto sO = [&](int i) { return smem + (2 + i) * C::QB; };
   const int tid = threadIdx.x, l = tid & 63, col = l & 31, h = l >> 5, wv = uniform(tid >> 6);
-  int tile, bk;
-  tile_and_head(a.ntk, a.B * a.Hkv, false, tile, bk);
+  int tile, bks;
+  tile_and_head(a.ntk, a.B * a.Hkv * a.nsk, false, tile, bks);
+  const int bk = bks / a.nsk, sp = bks % a.nsk;
   const int b = bk / a.Hkv, kh = bk % a.Hkv;
   const Seq sq = seq_of(a, b);
   const int j0 = tile * C::BK, jw = j0 + wv * 32, kj = jw + col;
-  const size_t krow = (size_t)bk * a.nk + min(kj, a.nk - 1);
+  const size_t first = ((size_t)bk * a.nk + min(kj, a.nk - 1)) * D;
   typename F::frag kf[D / F::KS], vf[D / F::KS];
-  row_frags<T, D>(kf, (const T*)a.k + krow * D);
+  row_frags<T, D>(kf, (const T*)a.k + first);
   if constexpr (C::VLDS) {                                // (each half-wave row is read by its own lane only)
-    row_frags<T, D>(vf, (const T*)a.v + krow * D);
+    row_frags<T, D>(vf, (const T*)a.v + first);
 #pragma unroll
     for (int i = 0; i < D / F::KS; ++i) *(typename F::frag*)(sV + (wv * 32 + col) * C::VST + i * F::KS + h * F::KPL) = vf[i];
   } else {
-    row_frags<T, D>(vf, (const T*)a.v + krow * D);
+    row_frags<T, D>(vf, (const T*)a.v + first);
   }
 
   // query rows that see any of the workgroup's keys
@@ -641,21 +683,24 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     i1 = a.window > 0 ? min(sq.lq, min(j0 + C::BK, sq.lk) - 1 - sq.off + a.window) : sq.lq;
   }
   const int t0 = i0 / QT, per = i1 > i0 ? (i1 - 1) / QT - t0 + 1 : 0;      // tiles per head
-  const int total = per * a.G;
+  // tiles of all heads of the group in turn, this workgroup's share of them
+  const int share = (per * a.G + a.nsk - 1) / a.nsk;
+  const int u0 = min(sp * share, per * a.G), total = min(share, per * a.G - u0);
 
   f32x16 dk[D / 32], dv[D / 32];
 #pragma unroll
   for (int dt = 0; dt < D / 32; ++dt) { dk[dt] = zero16(); dv[dt] = zero16(); }
-  StageRows<T, QT, D, C::NT> rq, ro;
+  TileRows<T, QT, D, C::NT> rq, ro;
   float rs = 0.0f;
   const float rc = 1.0f / a.c;
   // the tile that is loaded next: head g of the group, rows r
   const int rlast = (t0 + per - 1) * QT;
-  int lg = 0, lr = t0 * QT;
+  int lg = total > 0 ? u0 / per : 0, lr = (t0 + (total > 0 ? u0 % per : 0)) * QT;
+  int r0 = lr;
   auto load = [&]() {
     const size_t base = ((size_t)b * a.H + kh * a.G + lg) * a.nq;
-    rq.load((const T*)a.q + base * D, D, lr, 0, sq.lq, tid);
-    ro.load((const T*)a.dout + base * D, D, lr, 0, sq.lq, tid);
+    rq.load((const T*)a.q + base * D, lr, sq.lq, tid);
+    ro.load((const T*)a.dout + base * D, lr, sq.lq, tid);
     if (tid < 2 * QT) {
       const int r = min(lr + (tid & (QT - 1)), sq.lq - 1);
       const float x = tid < QT ? a.lse[base + r] : a.delta[base + r];
@@ -672,10 +717,9 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   };
   if (total > 0) {
     load();
-    stage(t0 * QT, 0);
+    stage(r0, 0);
     load();
   }
-  int r0 = t0 * QT;
 #pragma unroll 1
   for (int u = 0; u < total; ++u) {
     const int cur = u & 1, rn = r0 == rlast ? t0 * QT : r0 + QT, rr = r0;
@@ -724,7 +768,15 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
       for (int dt = 0; dt < D / 32; ++dt) dk[dt] = F::mma(F::tld_crow(sQ(cur), C::ST, 0, i, dt * 32), ds, dk[dt]);
     }
   }
-  if (kj < a.nk) {
+  if (kj >= a.nk) return;
+  int j = jw + (lane_id() & 31);
+  asm("" : "+v"(j));                                      // (the row's address made again, not kept through the loop)
+  const size_t krow = (size_t)bk * a.nk + j;
+  if (a.nsk > 1) {                                        // [2][ns][B][Hkv][nk][D]
+    const size_t rows = (size_t)a.B * a.Hkv * a.nk;
+    store_col<float, D>(a.part + ((size_t)sp * rows + krow) * D, dk, a.scale);
+    store_col<float, D>(a.part + ((size_t)(a.nsk + sp) * rows + krow) * D, dv, 1.0f);
+  } else {
     store_col<T, D>((T*)a.dk + krow * D, dk, a.scale);
     store_col<T, D>((T*)a.dv + krow * D, dv, 1.0f);
   }
@@ -805,19 +857,67 @@ static int run_fwd(const AttnShape& s, AttnArgs a, hipStream_t st) {
   return 0;
 }
 
+// Splits of the backward sweeps, as above: `groups` workgroups of `most` (`mean`)
+// tiles of 32 rows, `us` microseconds each; `bytes` of one partial result.
+static int sweep_splits(double groups, double most, double mean, double us, double bytes) {
+  int best = 1;
+  double best_t = 1e300;
+  for (int n = 1; n <= 32 && (n == 1 || n <= most); ++n) {
+    const double longest = (most / n + 4.0) * us, load = groups * n * (mean / n + 4.0) * us / 256;
+    double t = sqrt(longest * longest + load * load);
+    if (n > 1) t += 4.0 + 2.0 * n * bytes / 4e6;
+    if (t < 0.98 * best_t) { best_t = t; best = n; }
+  }
+  return best;
+}
+
+// A tile of 32 keys takes the query sweep 0.35 + 0.0035 D us (float32: 0.4 +
+// 0.065 D), a tile of 32 queries the key sweep 0.5 + 0.0053 D (0.4 + 0.09 D).
+// 12 heads on 6 key heads, 777 tokens, D = 32, float32: key sweep 57 -> 27 us.
+void attn_bwd_splits(const AttnShape& s, int* nsq, int* nsk) {
+  const double G = (double)(s.H / s.Hkv), D = s.D;
+  const bool half = s.dtype == 1;
+  double most = (double)s.nk, mean = (double)s.nk, kmost = (double)s.nq, kmean = (double)s.nq;
+  if (s.causal && s.nq <= s.nk) {
+    mean = (double)s.nk - 0.5 * (double)s.nq;
+    kmean = (double)s.nq * mean / (double)s.nk;
+  }
+  if (s.window > 0) {
+    const double w = (double)(s.window + 128);
+    most = most < w ? most : w; mean = mean < w ? mean : w;
+    kmost = kmost < w ? kmost : w; kmean = kmean < w ? kmean : w;
+  }
+  *nsq = sweep_splits((double)(s.B * s.H * ((s.nq + 127) / 128)), most / 32, mean / 32,
+                      half ? 0.35 + 0.0035 * D : 0.4 + 0.065 * D, (double)(s.B * s.H * s.nq) * D * 4);
+  *nsk = sweep_splits((double)(s.B * s.Hkv * ((s.nk + 127) / 128)), G * kmost / 32, G * kmean / 32,
+                      half ? 0.5 + 0.0053 * D : 0.4 + 0.09 * D, 2.0 * (double)(s.B * s.Hkv * s.nk) * D * 4);
+}
+
+template <typename T>
+static int run_sum(const float* part, void* out0, void* out1, size_t n, int ns, hipStream_t st) {
+  ProfScope ps("attn_sum", st);
+  k_attn_sum<T><<<dim3((unsigned)((n / 4 + 255) / 256), out1 ? 2 : 1), 256, 0, st>>>(part, (T*)out0, (T*)out1, n, ns);
+  return launch_status("attn sum");
+}
+
 template <typename T, int D>
 static int run_bwd(const AttnShape& s, AttnArgs a, hipStream_t st) {
+  const size_t nq = (size_t)s.B * s.H * s.nq * D, nk = (size_t)s.B * s.Hkv * s.nk * D;
   (void)hipGetLastError();
   {
     ProfScope ps("attn_dq", st);
-    k_attn_dq<T, D><<<(unsigned)(s.B * s.H * a.ntq), 256, 0, st>>>(a);
+    k_attn_dq<T, D><<<(unsigned)(s.B * s.H * a.nsq * a.ntq), 256, 0, st>>>(a);
   }
   if (int rc = launch_status("attn dq sweep")) return rc;
+  if (a.nsq > 1)
+    if (int rc = run_sum<T>(a.part, a.dq, nullptr, nq, a.nsq, st)) return rc;
   {
     ProfScope ps("attn_dkv", st);
-    k_attn_dkv<T, D><<<(unsigned)(s.B * s.Hkv * a.ntk), 256, 0, st>>>(a);
+    k_attn_dkv<T, D><<<(unsigned)(s.B * s.Hkv * a.nsk * a.ntk), 256, 0, st>>>(a);
   }
-  return launch_status("attn dk/dv sweep");
+  if (int rc = launch_status("attn dk/dv sweep")) return rc;
+  if (a.nsk == 1) return 0;
+  return run_sum<T>(a.part, a.dk, a.dv, nk, a.nsk, st);
 }
 
 #define ATTN_DISPATCH(FN)                                                        \

@@ -68,9 +68,9 @@ int check_attn(const linsimp_attn_dims* d, AttnShape* s) {
   return LINSIMP_OK;
 }
 
-// [ns][B][H][nq][D + 2] partial results, then (backward) delta [B][H][nq]
-size_t attn_ws(const AttnShape& s, int ns, bool backward, AttnArgs* a, void* base) {
+size_t attn_fwd_ws(const AttnShape& s, AttnArgs* a, void* base) {
   const size_t rows = (size_t)s.B * s.H * s.nq;
+  const int ns = attn_splits(s);
   size_t off = 0;
   auto take = [&](size_t bytes) {
     void* p = base ? (char*)base + off : nullptr;
@@ -79,10 +79,19 @@ size_t attn_ws(const AttnShape& s, int ns, bool backward, AttnArgs* a, void* bas
   };
   float* part = ns > 1 ? take((size_t)ns * rows * s.D * 4) : nullptr;
   float* pml = ns > 1 ? take((size_t)ns * rows * 2 * 4) : nullptr;
-  if (backward) off = 0;                                 // the backward needs no partial results
-  float* delta = backward ? take(rows * 4) : nullptr;
-  if (a) { a->part = part; a->pml = pml; a->delta = delta; }
+  if (a) { a->ns = ns; a->part = part; a->pml = pml; }
   return off > 256 ? off : 256;
+}
+
+// delta, then the splits' gradients: dq's are summed before the key sweep writes its own
+size_t attn_bwd_ws(const AttnShape& s, AttnArgs* a, void* base) {
+  const size_t qe = (size_t)s.B * s.H * s.nq * s.D * 4, ke = (size_t)s.B * s.Hkv * s.nk * s.D * 4;
+  const size_t delta = al((size_t)s.B * s.H * s.nq * 4);
+  int nsq, nsk;
+  attn_bwd_splits(s, &nsq, &nsk);
+  const size_t pq = nsq > 1 ? nsq * qe : 0, pk = nsk > 1 ? 2 * nsk * ke : 0;
+  if (a) { a->nsq = nsq; a->nsk = nsk; a->delta = (float*)base; a->part = (float*)((char*)base + delta); }
+  return delta + al(pq > pk ? pq : pk);
 }
 
 AttnArgs attn_args(const AttnShape& s) {
@@ -90,7 +99,7 @@ AttnArgs attn_args(const AttnShape& s) {
   a.B = (int)s.B; a.H = (int)s.H; a.Hkv = (int)s.Hkv; a.G = (int)(s.H / s.Hkv);
   a.nq = (int)s.nq; a.nk = (int)s.nk; a.causal = s.causal; a.window = (int)s.window;
   a.ntq = (int)((s.nq + 127) / 128); a.ntk = (int)((s.nk + 127) / 128);
-  a.ns = 1; a.scale = s.scale; a.c = s.scale * 1.4426950408889634f;
+  a.ns = a.nsq = a.nsk = 1; a.scale = s.scale; a.c = s.scale * 1.4426950408889634f;
   return a;
 }
 
@@ -146,8 +155,8 @@ extern "C" {
 size_t linsimp_attn_workspace_size(const linsimp_attn_dims* dims, int for_backward) {
   AttnShape s;
   if (check_attn(dims, &s) != LINSIMP_OK) return 0;
-  const size_t fwd = attn_ws(s, attn_splits(s), false, nullptr, nullptr);
-  const size_t bwd = for_backward ? attn_ws(s, 1, true, nullptr, nullptr) : 0;
+  const size_t fwd = attn_fwd_ws(s, nullptr, nullptr);
+  const size_t bwd = for_backward ? attn_bwd_ws(s, nullptr, nullptr) : 0;
   return fwd > bwd ? fwd : bwd;
 }
 
@@ -161,11 +170,10 @@ int linsimp_attn_fwd(const linsimp_attn_dims* dims, const void* q, const void* k
   if ((rc = check_ptrs("q,k,v,out", ps, 4))) return rc;
   if ((rc = check_opt("lens_q", lens_q, 3)) || (rc = check_opt("lens_k", lens_k, 3)) || (rc = check_opt("lse", lse, 15)))
     return rc;
-  const int ns = attn_splits(s);
-  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_ws(s, ns, false, nullptr, nullptr)))) return rc;
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_fwd_ws(s, nullptr, nullptr)))) return rc;
   AttnArgs a = attn_args(s);
-  a.q = q; a.k = k; a.v = v; a.lens_q = lens_q; a.lens_k = lens_k; a.out = out; a.lse = lse; a.ns = ns;
-  attn_ws(s, ns, false, &a, workspace);
+  a.q = q; a.k = k; a.v = v; a.lens_q = lens_q; a.lens_k = lens_k; a.out = out; a.lse = lse;
+  attn_fwd_ws(s, &a, workspace);
   return launch_attn_fwd(s, a, (hipStream_t)stream);
 }
 
@@ -179,11 +187,11 @@ int linsimp_attn_bwd(const linsimp_attn_dims* dims, const void* q, const void* k
   const void* ps[] = {q, k, v, out, lse, dout, dq, dk, dv};
   if ((rc = check_ptrs("q,k,v,out,lse,dout,dq,dk,dv", ps, 9))) return rc;
   if ((rc = check_opt("lens_q", lens_q, 3)) || (rc = check_opt("lens_k", lens_k, 3))) return rc;
-  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_ws(s, 1, true, nullptr, nullptr)))) return rc;
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_bwd_ws(s, nullptr, nullptr)))) return rc;
   AttnArgs a = attn_args(s);
   a.q = q; a.k = k; a.v = v; a.lens_q = lens_q; a.lens_k = lens_k;
   a.out = (void*)out; a.lse = (float*)lse; a.dout = dout; a.dq = dq; a.dk = dk; a.dv = dv;
-  attn_ws(s, 1, true, &a, workspace);
+  attn_bwd_ws(s, &a, workspace);
   return launch_attn_bwd(s, a, (hipStream_t)stream);
 }
 
@@ -199,11 +207,10 @@ int linsimp_attn_step(const linsimp_attn_dims* dims, const void* q, const void* 
   }
   const void* ps[] = {q, k, v, kcache, vcache, pos, out};
   if ((rc = check_ptrs("q,k,v,kcache,vcache,pos,out", ps, 7))) return rc;
-  const int ns = attn_splits(s);
-  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_ws(s, ns, false, nullptr, nullptr)))) return rc;
+  if ((rc = check_buf("workspace", workspace, workspace_bytes, attn_fwd_ws(s, nullptr, nullptr)))) return rc;
   AttnArgs a = attn_args(s);
-  a.q = q; a.k = kcache; a.v = vcache; a.knew = k; a.vnew = v; a.pos = pos; a.out = out; a.ns = ns;
-  attn_ws(s, ns, false, &a, workspace);
+  a.q = q; a.k = kcache; a.v = vcache; a.knew = k; a.vnew = v; a.pos = pos; a.out = out;
+  attn_fwd_ws(s, &a, workspace);
   return launch_attn_fwd(s, a, (hipStream_t)stream);
 }
 
