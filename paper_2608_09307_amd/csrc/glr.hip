@@ -252,18 +252,25 @@ LS_DEV void get_vec(int l, const float* src, float (&x)[16]) {
 // (REV: the last, then the first).  lo, lack, lack', fz: the wave's 32 floats each.
 // Returns whether the channels allow the short way (a cleared channel's sums
 // come out as NaN and do not).
+template <typename T> struct Picks {                    // of every chunk: made once
+  typename MF<T>::frag mid[GlrBase<T>::NKS], one;
+  LS_DEV void init(int l) {
+#pragma unroll
+    for (int ks = 0; ks < GlrBase<T>::NKS; ++ks) mid[ks] = ones_where<T>(l, ks, Middle{});
+    one = ones_where<T>(l, 0, All{});
+  }
+};
 template <typename T, bool REV>
-LS_DEV bool gate_chunk(int l, const T* sg, f32x16& E, float* lo, const float* lack, float* next, float* fz) {
+LS_DEV bool gate_chunk(int l, const Picks<T>& pick, const T* sg, f32x16& E, float* lo, const float* lack, float* next, float* fz) {
   using F = MF<T>;
   constexpr int NKS = GlrBase<T>::NKS, WST = GlrBase<T>::WST;
   f32x16 first = zero16();
   E = zero16();
-  const typename F::frag one = ones_where<T>(l, 0, All{});
 #pragma unroll
   for (int ks = 0; ks < NKS; ++ks) {
     const typename F::frag x = rows_nat<true>(l, sg, WST, ks, 0);
-    E = F::mma(x, ones_where<T>(l, ks, Middle{}), E);
-    if (ks < NKS / 2) first = F::mma(x, one, first);
+    E = F::mma(x, pick.mid[ks], E);
+    if (ks < NKS / 2) first = F::mma(x, pick.one, first);
   }
   put_vec(l, 0, REV ? next : lo, first);
   put_vec(l, 31, REV ? lo : next, E);                  // (row 31's sum from the middle: the last 16 rows)
@@ -322,9 +329,9 @@ template <typename T> LS_DEV void put_decayed(int l, T* hi, T* lo, int ld, const
   put_scaled(l, hi, lo, ld, x, f, low);
 }
 
-// the rows of level L of the exact way (0: the rows as they are)
+// the rows of level L of the exact way (0: the rows as they are); returns its sums of g
 template <typename T>
-LS_DEV void put_level(int l, int L, const T* sg, T* dq, T* dk, int ld, const Row16<T>& xq, const Row16<T>& xk, float scale) {
+LS_DEV f32x16 put_level(int l, int L, const T* sg, T* dq, T* dk, int ld, const Row16<T>& xq, const Row16<T>& xk, float scale) {
   const f32x16 B = gate_sum(l, sg, Border{L ? L : 32});
   const bool later = (l & L) != 0;
   float f[16];
@@ -334,6 +341,7 @@ LS_DEV void put_level(int l, int L, const T* sg, T* dq, T* dk, int ld, const Row
 #pragma unroll
   for (int v = 0; v < 16; ++v) f[v] = L == 0 ? 1.0f : later ? 0.0f : ex(B[v]);
   put_scaled(l, dk, dk, ld, xk.again(), f, false);
+  return B;
 }
 
 // a 32 x 32 tile as the next product's operand, all of it and with the elements (row, column) that f keeps
@@ -449,6 +457,8 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
   // spend[c & 1]: the log decay that S still lacks before chunk c
   if (tid < D) spend[c0 & 1][tid] = 0.0f;
   __syncthreads();
+  Picks<T> pick;
+  pick.init(l);
   Row16<T> rq, rk, rg, rv;
   auto load = [&](int c) {
     const size_t at = base + (size_t)32 * c * D;
@@ -470,7 +480,7 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
     wave_lds_sync();
     {
       f32x16 E;
-      const bool fast = gate_chunk<T, false>(l, sg, E, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w);
+      const bool fast = gate_chunk<T, false>(l, pick, sg, E, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w);
       put_decayed(l, sQ(i) + 32 * w, sQ(i), ST, rq, E, 1.0f, a.scale, false);
       put_decayed(l, sK(i) + 32 * w, sL(i) + 32 * w, ST, rk, E, -1.0f, 1.0f, a.exact);
       if (l == 0) sslow[i][w] = !fast;
@@ -618,6 +628,8 @@ LS_DEV void glr_walk(const GlrArgs& a, T* smem, float* svec, int (*sslow)[D / 32
   float *vec = svec + w * 160, *vlo = vec + 64, *vfz = vec + 96, *vall = vec + 128;
   if (l < 32) vec[l] = 0.0f;
   float total = 0.0f;                                    // log decay across the rows so far, of channel 32 w + l (l < 32)
+  Picks<T> pick;
+  pick.init(l);
   Row16<T> rk, rg, rv;
   auto load = [&](int c) {
     const size_t at = base + (size_t)32 * c * D;
@@ -638,7 +650,7 @@ LS_DEV void glr_walk(const GlrArgs& a, T* smem, float* svec, int (*sslow)[D / 32
     const Row16<T> xk = rk;
     {
       f32x16 E;
-      const bool fast = gate_chunk<T, REV>(l, sg, E, vlo, vec + 32 * i, vec + 32 * (i ^ 1), vfz);
+      const bool fast = gate_chunk<T, REV>(l, pick, sg, E, vlo, vec + 32 * i, vec + 32 * (i ^ 1), vfz);
       put_decayed(l, sk, sl, WST, rk, E, REV ? 1.0f : -1.0f, sc, a.exact);
       if (l == 0) sslow[i][w] = !fast;
     }
@@ -991,7 +1003,7 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 #pragma unroll 1
         for (int L = 0; L <= 16; L = L ? 2 * L : 1) {            // (L = 0, the diagonal: for the value waves)
           __syncthreads();
-          put_level(l, L, sg, sQ(i) + 32 * w, sK(i) + 32 * w, ST, xq, xk, a.scale);
+          const f32x16 B = put_level(l, L, sg, sQ(i) + 32 * w, sK(i) + 32 * w, ST, xq, xk, a.scale);
           __syncthreads();
           f32x16 bq = zero16(), bk = zero16();
 #pragma unroll
@@ -1001,7 +1013,6 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
             bk = F::mma(rows_crow<true>(l, sQ(i), ST, sp, 32 * w),
                         dP.keep(l, sp, [L](int t_, int s) { return L != 0 && joins(L, s, t_); }), bk);
           }
-          const f32x16 B = gate_sum(l, sg, Border{L ? L : 32});
           float y[16];
           get_row(qme, y);
 #pragma unroll
@@ -1060,6 +1071,8 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
     load_state<NW>(l, R, src, D, 32 * w + chan_of(col));
     // They also scale the key rows: while the key waves work on chunk c, chunk c - 1
     // is staged, from rows loaded a chunk earlier.
+    Picks<T> pick;
+    pick.init(l);
     Row16<T> rq, rk, rg, rv, ro;
     auto load = [&](int c) {
       const size_t at = base + (size_t)32 * c * D;
@@ -1077,7 +1090,7 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
       put_row(sO(i) + col * ST + 32 * w + 16 * h, ro);
       wave_lds_sync();
       f32x16 E;
-      const bool fast = gate_chunk<T, true>(l, sG(i), E, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w);
+      const bool fast = gate_chunk<T, true>(l, pick, sG(i), E, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w);
       put_decayed(l, sK(i) + 32 * w, sK(i), ST, rk, E, -1.0f, 1.0f, false);
       float f[16];
 #pragma unroll
