@@ -26,7 +26,8 @@ struct GlrArgs {
   float *part, *rpart;                    // [BH][G][D*D]
   float *fac, *rfac;                      // [BH][G][D]
   int* again;                             // [BH][G] whether a segment has a chunk for the exact way
-  void* states;                           // [BH][nch][D*D] operand type, fragment order (backward)
+  void* states;                           // backward: [BH][nch][D*D] operand type, fragment order
+  float* pre;                             // backward, G > 1: [BH][nch][D] log decay from the segment's start to each
   int H, n, nch, G, cps;                  // chunks of 32 rows in all, segments, chunks per segment
   int exact;                              // keep the low half of the rounded keys (a float32 state is asked for)
   float scale;

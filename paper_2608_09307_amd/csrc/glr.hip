@@ -590,9 +590,10 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 // register per lane and its scaled rows are the wave's own.
 //   REV = false  S over a segment's rows, from k and v
 //   REV = true   R backwards over a segment's rows, from q and do
-//   STORE        from the segment's start state: Z of every chunk (S_start on
-//                the exact way) as operand fragments for the backward
-//   otherwise    from zero: the segment's own part and the decay across it
+// From zero, to the segment's own part and the decay across it.  STORE: also Z of
+// every chunk (S_start on the exact way) as operand fragments for the backward,
+// which adds what the segment's start state, decayed by `pre`, contributes; a
+// single segment starts from s0 itself.
 // ---------------------------------------------------------------------------
 template <typename T, int D> struct GlrWalk {
   static constexpr int NW = D / 32, NT = 64 * NW;
@@ -620,8 +621,7 @@ LS_DEV void glr_walk(const GlrArgs& a, T* smem, float* svec, int (*sslow)[D / 32
 
   f32x16 S[NW];
   {
-    const float* src = !STORE ? nullptr : a.G > 1 ? a.part + ((size_t)bh * a.G + seg) * D * D
-                                        : a.s0 ? a.s0 + (size_t)bh * D * D : nullptr;
+    const float* src = STORE && a.G == 1 && a.s0 ? a.s0 + (size_t)bh * D * D : nullptr;
     load_state_t<NW>(l, S, src ? src + (size_t)me * D : nullptr);
   }
   // this wave's vectors: lack (two chunks), sums, scaling, decay across the chunk
@@ -660,6 +660,8 @@ LS_DEV void glr_walk(const GlrArgs& a, T* smem, float* svec, int (*sslow)[D / 32
 #pragma unroll
     for (int x = 0; x < NW; ++x) slow = slow || sslow[i][x];
     slow = uniform((int)slow);
+    if (STORE && a.G > 1 && l < 32)                      // the decay from the segment's start to what is stored
+      a.pre[((size_t)bh * a.nch + c) * D + 32 * w + l] = total + (slow ? 0.0f : vlo[l]);
     if (__builtin_expect(!slow, 1)) {
       if (l < 32) total += vlo[l] + vec[32 * (i ^ 1) + l];
     } else {
@@ -703,7 +705,7 @@ LS_DEV void glr_walk(const GlrArgs& a, T* smem, float* svec, int (*sslow)[D / 32
       }
     }
   }
-  if constexpr (!STORE) {
+  if (!STORE || seg < a.G - 1) {
     wave_lds_sync();
     if (l < 32) (REV ? a.rfac : a.fac)[((size_t)bh * a.G + seg) * D + 32 * w + l] = ex(total);
     const float zc = ex(vec[32 * ((cl - c0) & 1) + chan_of(col)]);
@@ -717,21 +719,17 @@ LS_DEV void glr_walk(const GlrArgs& a, T* smem, float* svec, int (*sslow)[D / 32
   }
 }
 
-// blockIdx.y: forward parts, then (backward) reverse parts
-template <typename T, int D, bool STORE>
+// The segments' own parts (the last segment adds to no later one; reversed, the
+// first to no earlier one), for the backward with every chunk's Z.
+template <typename T, int D, bool BWD>
 __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void k_glr_walk(GlrArgs a) {
   using C = GlrWalk<T, D>;
   __shared__ __align__(16) T smem[C::ELEMS];
   __shared__ __align__(16) float svec[C::NW * 160];
   __shared__ int sslow[2][C::NW];
-  if constexpr (STORE) {
-    glr_walk<T, D, false, true>(a, smem, svec, sslow, blockIdx.x / a.G, blockIdx.x % a.G);
-  } else {
-    // the last segment adds to no later one (reverse: the first to no earlier one)
-    const int bh = blockIdx.x / (a.G - 1), s = blockIdx.x % (a.G - 1);
-    if (blockIdx.y == 0) glr_walk<T, D, false, false>(a, smem, svec, sslow, bh, s);
-    else glr_walk<T, D, true, false>(a, smem, svec, sslow, bh, s + 1);
-  }
+  const int segs = BWD ? a.G : a.G - 1, bh = blockIdx.x / segs, seg = blockIdx.x % segs;
+  if (blockIdx.y == 0) glr_walk<T, D, false, BWD>(a, smem, svec, sslow, bh, seg);
+  else if (BWD && seg > 0) glr_walk<T, D, true, false>(a, smem, svec, sslow, bh, seg);
 }
 
 // The state that every segment starts from, in the place of its part: four
@@ -853,6 +851,15 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
   if (keys) {
     const int me = 32 * w + chan_of(col);
     load_state_t<NW>(l, R, src ? src + (size_t)me * D : nullptr);
+    // the segment's start state, which the stored Z lack
+    const bool start = a.G > 1 && (seg > 0 || a.s0 != nullptr);
+    Tile<T> z0[NW];
+    {
+      f32x16 x[NW];
+      load_state_t<NW>(l, x, start ? a.part + (((size_t)bh * a.G + seg) * D + me) * D : nullptr);
+#pragma unroll
+      for (int et = 0; et < NW; ++et) z0[et].set(x[et]);
+    }
 #pragma unroll 1
     for (int c = cl - 1; c >= c0; --c) {
       l = lane_in(lane, c); col = l & 31; h = l >> 5;
@@ -866,6 +873,8 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
         xq.load(lane_ptr((const T*)a.q + at, off)); xk.load(lane_ptr((const T*)a.k + at, off));
       };
       const typename F::frag* zs = (const typename F::frag*)a.states + (((size_t)bh * a.nch + c) * NW + w) * NW * F::CSTEPS * 64 + (unsigned)l;
+      float decay = kNegInf;                             // of the start state, channel 32 w + (l & 31); log
+      if (start) decay = a.pre[((size_t)bh * a.nch + c) * D + 32 * w + (unsigned)(l & 31)];
       typename F::frag z[NW][F::CSTEPS];                // Z of this chunk, on its way before the barrier
 #pragma unroll
       for (int et = 0; et < NW; ++et)
@@ -900,7 +909,8 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
         dP.set(p);
       };
       auto outside = [&](float zc, auto with_pairs) {
-        f32x16 pt = zero16(), p = zero16();
+        f32x16 pt = zero16(), p = zero16(), a0 = zero16();
+        float t0 = 0.0f;
 #pragma unroll
         for (int et = 0; et < NW; ++et) {
           R[et] *= zc;
@@ -913,13 +923,25 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
             }
             const typename F::frag r = F::cfrag(R[et], sp);
             through = dot_add(r, z[et][sp], through);
+            t0 = dot_add(r, z0[et].f[sp], t0);
             aq = F::mma(z[et][sp], of, aq);
             ak = F::mma(r, vf, ak);
+            a0 = F::mma(z0[et].f[sp], of, a0);
           }
           __builtin_amdgcn_sched_barrier(0);             // (one tile's operands in registers at a time)
         }
-        through = half_swap_add(through);
         if constexpr (decltype(with_pairs)::value) keep_pairs(pt, p);
+        // what the segment's start state adds (without one: zeros)
+        __builtin_amdgcn_sched_barrier(0);
+        float y[16];
+        if (h == 0) sw[32 * w + (l & 31)] = ex(decay);
+        wave_lds_sync();
+        get_vec(l, sw + 32 * w, y);
+        through = __builtin_fmaf(sw[me], t0, through);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) aq[v] = __builtin_fmaf(y[v], a0[v], aq[v]);
+        wave_lds_sync();
+        through = half_swap_add(through);
       };
       // W into sw: what passes through the chunk, and the pairs that start in it and end after it
       auto put_w = [&]() {
@@ -1255,21 +1277,23 @@ int glr_segments(const GlrShape& s, bool backward) {
   return best;
 }
 
-template <typename T, int D> static int run_parts(const GlrShape& s, const GlrArgs& a, bool backward, hipStream_t st) {
+template <typename T, int D, bool BWD> static int run_parts(const GlrShape& s, const GlrArgs& a, hipStream_t st) {
   {
-    ProfScope ps("glr_parts", st);
-    k_glr_walk<T, D, false><<<dim3((unsigned)(s.BH() * (a.G - 1)), backward ? 2 : 1), 2 * D, 0, st>>>(a);
+    const dim3 grid((unsigned)(s.BH() * (BWD ? a.G : a.G - 1)), BWD && a.G > 1 ? 2 : 1);
+    ProfScope ps(BWD ? "glr_states" : "glr_parts", st);
+    k_glr_walk<T, D, BWD><<<grid, 2 * D, 0, st>>>(a);
   }
   if (int rc = launch_status("glr parts")) return rc;
+  if (a.G == 1) return 0;
   ProfScope ps("glr_scan", st);
-  k_glr_scan<D><<<dim3((D * D / 4 + 255) / 256, (unsigned)s.BH(), backward ? 2 : 1), 256, 0, st>>>(a);
+  k_glr_scan<D><<<dim3((D * D / 4 + 255) / 256, (unsigned)s.BH(), BWD ? 2 : 1), 256, 0, st>>>(a);
   return launch_status("glr scan");
 }
 
 template <typename T, int D> static int run_fwd(const GlrShape& s, const GlrArgs& a, hipStream_t st) {
   (void)hipGetLastError();
   if (a.G > 1)
-    if (int rc = run_parts<T, D>(s, a, false, st)) return rc;
+    if (int rc = run_parts<T, D, false>(s, a, st)) return rc;
   ProfScope ps("glr_fwd", st);
   k_glr_fwd<T, D, false><<<(unsigned)(s.BH() * a.G), 2 * D, 0, st>>>(a);
   k_glr_fwd<T, D, true><<<(unsigned)(s.BH() * a.G), 2 * D, 0, st>>>(a);
@@ -1278,13 +1302,7 @@ template <typename T, int D> static int run_fwd(const GlrShape& s, const GlrArgs
 
 template <typename T, int D> static int run_bwd(const GlrShape& s, const GlrArgs& a, hipStream_t st) {
   (void)hipGetLastError();
-  if (a.G > 1)
-    if (int rc = run_parts<T, D>(s, a, true, st)) return rc;
-  {
-    ProfScope ps("glr_states", st);
-    k_glr_walk<T, D, true><<<(unsigned)(s.BH() * a.G), 2 * D, 0, st>>>(a);
-  }
-  if (int rc = launch_status("glr states")) return rc;
+  if (int rc = run_parts<T, D, true>(s, a, st)) return rc;
   ProfScope ps("glr_bwd", st);
   const unsigned grid = (unsigned)(s.BH() * a.G);
   if (sizeof(T) == 2 && a.exact) {

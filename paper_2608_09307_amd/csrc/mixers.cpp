@@ -136,7 +136,8 @@ size_t glr_ws(const GlrShape& s, int G, bool backward, GlrArgs* a, void* base) {
   float* rpart = G > 1 && backward ? (float*)take(BH * G * DD * 4) : nullptr;
   float* rfac = G > 1 && backward ? (float*)take(BH * G * s.D * 4) : nullptr;
   void* states = backward ? take(BH * (size_t)s.nch() * DD * s.esize()) : nullptr;
-  if (a) { a->again = again; a->part = part; a->fac = fac; a->rpart = rpart; a->rfac = rfac; a->states = states; }
+  float* pre = G > 1 && backward ? (float*)take(BH * (size_t)s.nch() * s.D * 4) : nullptr;
+  if (a) { a->pre = pre; a->again = again; a->part = part; a->fac = fac; a->rpart = rpart; a->rfac = rfac; a->states = states; }
   return off;
 }
 
