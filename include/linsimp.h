@@ -213,7 +213,10 @@ int linsimp_decode_chunk(int64_t S, int32_t H, int32_t T, int32_t D, int32_t Dv,
  * above: dense [B, heads, rows, D] device tensors, 16-byte aligned, the
  * caller's workspace (256-byte aligned), calls that only enqueue on `stream`,
  * negative statuses.  D is 32, 64 or 128 with LINSIMP_BF16 and 32 or 64 with
- * LINSIMP_F32.  Results are the same bits on every run of a call. */
+ * LINSIMP_F32.  Results are the same bits on every run of a call.  Sizes:
+ * attention B*H <= 2^20, B*H*nq <= 2^30, nk <= 2^30, and for the backward
+ * B*Hkv*nk <= 2^30; recurrence B*H <= 65535 (the step 2^24 - 1), B*H*n <= 2^31.
+ * Outputs must not overlap inputs, but where it is said that they may. */
 
 typedef struct {
   int64_t B;       /* batch (sequences)                                       */
@@ -225,7 +228,7 @@ typedef struct {
   int32_t D;       /* width of q, k, v, out                                   */
   int32_t dtype;   /* linsimp_dtype                                           */
   int32_t causal;  /* 1: no query sees a later key; 0: every key              */
-  float scale;     /* > 0; D^-1/2 in the usual layer                          */
+  float scale;     /* 1e-18 .. 1e18; D^-1/2 in the usual layer                */
 } linsimp_attn_dims;
 
 /* Bytes of workspace linsimp_attn_fwd or linsimp_attn_step (for_backward = 0)

@@ -397,7 +397,7 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (STEP) {
     const int64_t p = a.pos[b];
     sq.lq = p < 0 ? 0 : 1;
-    sq.lk = p < 0 ? 0 : (int)(p + 1 < (int64_t)a.nk ? p + 1 : a.nk);
+    sq.lk = p < 0 ? 0 : p < (int64_t)a.nk ? (int)p + 1 : a.nk;
     slot = p < 0 ? -1 : (int)(p % a.nk);
     sq.off = sq.lk - sq.lq; sq.causal = 0; sq.window = 0;
     lo = 0; hi = sq.lk;
@@ -821,7 +821,7 @@ int attn_splits(const AttnShape& s) {
   const double partial = (double)(s.B * s.H * s.nq) * (s.D + 2) * 4.0;
   int best = 1;
   double best_t = 1e300;
-  for (int n = 1; n <= kMaxSplits && (n == 1 || n * tile < most + tile); ++n) {
+  for (int n = 1; n <= kMaxSplits && (n == 1 || (n * tile < most + tile && groups * n < 65536)); ++n) {
     const double longest = (most / tile / n + (few ? 1.5 : 3.0)) * us;
     const double load = few ? groups * mean * bytes / 5e6 + groups * n * 2.0 * us / 512
                             : groups * n * (mean / tile / n + 3.0) * us * 0.9 / 256;
@@ -862,7 +862,7 @@ static int run_fwd(const AttnShape& s, AttnArgs a, hipStream_t st) {
 static int sweep_splits(double groups, double most, double mean, double us, double bytes) {
   int best = 1;
   double best_t = 1e300;
-  for (int n = 1; n <= 32 && (n == 1 || n <= most); ++n) {
+  for (int n = 1; n <= 32 && (n == 1 || (n <= most && groups * n < 65536)); ++n) {
     const double longest = (most / n + 4.0) * us, load = groups * n * (mean / n + 4.0) * us / 256;
     double t = sqrt(longest * longest + load * load);
     if (n > 1) t += 4.0 + 2.0 * n * bytes / 4e6;

@@ -1266,7 +1266,7 @@ int glr_segments(const GlrShape& s, bool backward) {
   const double kEnds = 2.0, kWalk = backward ? 0.7 : 0.6, kLaunch = backward ? 4.0 : 6.0;
   int best = 1;
   double best_t = 1e300;
-  for (int64_t G = 1; G <= 256 && G <= nch; ++G) {
+  for (int64_t G = 1; G <= 256 && G <= nch && (G == 1 || BH * G < 65536); ++G) {
     const int64_t cps = (nch + G - 1) / G;
     if ((nch + cps - 1) / cps != G) continue;                  // the last segment would be empty
     const double rounds = (double)((BH * G + slots - 1) / slots);

@@ -50,8 +50,8 @@ int check_attn(const linsimp_attn_dims* d, AttnShape* s) {
     set_error("attn: window must be >= 0, and 0 without causal");
     return LINSIMP_E_INVALID_ARG;
   }
-  if (!(d->scale > 0.0f) || !isfinite(d->scale)) {
-    set_error("attn: scale must be positive and finite");
+  if (!(d->scale >= 1e-18f && d->scale <= 1e18f)) {
+    set_error("attn: scale must be between 1e-18 and 1e18");
     return LINSIMP_E_INVALID_ARG;
   }
   // rows and slots are 32-bit within a head, and a grid has fewer than 2^32 threads
@@ -66,6 +66,13 @@ int check_attn(const linsimp_attn_dims* d, AttnShape* s) {
   s->window = d->window >= d->nk ? 0 : d->window;      // (no query then loses a key to it)
   s->D = d->D; s->dtype = d->dtype; s->causal = d->causal; s->scale = d->scale;
   return LINSIMP_OK;
+}
+
+// the key sweep's grid: a workgroup for every 128 keys
+int check_attn_bwd(const AttnShape& s) {
+  if (s.B * s.Hkv * s.nk <= (int64_t)1 << 30) return LINSIMP_OK;
+  set_error("attn backward: B*Hkv*nk=%lld is above 2^30", (long long)(s.B * s.Hkv * s.nk));
+  return LINSIMP_E_UNSUPPORTED;
 }
 
 size_t attn_fwd_ws(const AttnShape& s, AttnArgs* a, void* base) {
@@ -155,7 +162,7 @@ extern "C" {
 
 size_t linsimp_attn_workspace_size(const linsimp_attn_dims* dims, int for_backward) {
   AttnShape s;
-  if (check_attn(dims, &s) != LINSIMP_OK) return 0;
+  if (check_attn(dims, &s) != LINSIMP_OK || (for_backward && check_attn_bwd(s) != LINSIMP_OK)) return 0;
   const size_t fwd = attn_fwd_ws(s, nullptr, nullptr);
   const size_t bwd = for_backward ? attn_bwd_ws(s, nullptr, nullptr) : 0;
   return fwd > bwd ? fwd : bwd;
@@ -184,6 +191,7 @@ int linsimp_attn_bwd(const linsimp_attn_dims* dims, const void* q, const void* k
                      void* workspace, size_t workspace_bytes, void* stream) {
   AttnShape s;
   int rc = check_attn(dims, &s);
+  if (!rc) rc = check_attn_bwd(s);
   if (rc) return rc;
   const void* ps[] = {q, k, v, out, lse, dout, dq, dk, dv};
   if ((rc = check_ptrs("q,k,v,out,lse,dout,dq,dk,dv", ps, 9))) return rc;
