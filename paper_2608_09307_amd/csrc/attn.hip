@@ -31,7 +31,9 @@ struct Seq {
   int lq, lk, off, causal, window;
   LS_DEV int lo(int i) const { return window > 0 ? max(0, i + off - window + 1) : 0; }
   LS_DEV int hi(int i) const { return causal ? min(lk - 1, i + off) : lk - 1; }
-  LS_DEV bool sees(int i, int j) const { return j >= lo(i) && j <= hi(i) && i < lq; }
+  // the queries that see key j: first(j) <= i <= last(j)
+  LS_DEV int first(int j) const { return j >= lk ? lq : causal ? j - off : 0; }
+  LS_DEV int last(int j) const { return window > 0 ? min(lq - 1, j - off + window - 1) : lq - 1; }
 };
 
 LS_DEV Seq seq_of(const AttnArgs& a, int b) {
@@ -63,6 +65,30 @@ LS_DEV void tile_and_head(int nt, int heads, bool late_first, int& tile, int& he
   tile = late_first ? nt - 1 - t : t;
 }
 
+// Row padding of the backward's tiles, which are read by rows and transposed: a
+// pitch of 80 or 208 bytes modulo 256 (16 heads of 16k tokens, D = 128: key sweep
+// 2.38 -> 2.20 ms, query sweep 1.57 -> 1.51 against tr_pad's pitch, at which the
+// row reads conflict; 16 or 48 bytes: 2.36 and 2.25; 32: 2.24).
+template <typename T, int N> constexpr int both_pad() {
+  if (sizeof(T) != 2) return 1;
+  for (int p = 0; p < 128; p += 8) {
+    const int b = (2 * (N + p)) % 256;
+    if (b == 80 || b == 208) return p;
+  }
+  return 8;
+}
+
+// 16 bytes of a row to LDS, whole where the rows are laid out in 16-byte steps
+template <typename T, typename V>
+LS_DEV void put_piece(T* at, int lstride, V x) {
+  if ((lstride * (int)sizeof(T)) % 16 == 0) {
+    *(V*)at = x;
+  } else {
+#pragma unroll
+    for (int e = 0; e < 16 / (int)sizeof(T); ++e) at[e] = x[e];
+  }
+}
+
 // Staging of row tiles (common.h) with one address for the workgroup and an offset
 // in 32 bits per lane: rows row0 .. of a dense [*, COLS] matrix of `rows` rows,
 // those past its end read from its last one (and staged as zeros).
@@ -77,6 +103,21 @@ struct TileRows : StageRows<T, ROWS, COLS, NT> {
       const int idx = min(tid + NT * it, S::N - 1);
       const unsigned off = (unsigned)((min(idx / S::CPR, last) * COLS + (idx % S::CPR) * S::VE) * (int)sizeof(T));
       this->x[it] = *(const typename S::V*)(base + off);
+    }
+  }
+  // rows from hi on become zeros, in the one tile that has them: a select for each
+  // value of every tile was a quarter of the forward's instructions at D = 64
+  LS_DEV void store(T* lds, int lstride, int row0, int hi, int tid) {
+    if (row0 + ROWS > hi) {
+#pragma unroll
+      for (int it = 0; it < S::IT; ++it)
+        if (row0 + (tid + NT * it) / S::CPR >= hi) this->x[it] = typename S::V{};
+    }
+#pragma unroll
+    for (int it = 0; it < S::IT; ++it) {
+      const int idx = tid + NT * it;
+      if (S::N % NT != 0 && idx >= S::N) continue;
+      put_piece(lds + (idx / S::CPR) * lstride + (idx % S::CPR) * S::VE, lstride, this->x[it]);
     }
   }
 };
@@ -213,8 +254,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (t0 < t1) {
     rk.load(ks, t0 * KT, sq.lk, tid);
     rv.load(vs, t0 * KT, sq.lk, tid);
-    rk.store(sK(0), C::KST, t0 * KT, 0, sq.lk, tid);
-    rv.store(sV(0), C::VST, t0 * KT, 0, sq.lk, tid);
+    rk.store(sK(0), C::KST, t0 * KT, sq.lk, tid);
+    rv.store(sV(0), C::VST, t0 * KT, sq.lk, tid);
     rk.load(ks, (t0 + 1) * KT, sq.lk, tid);
     rv.load(vs, (t0 + 1) * KT, sq.lk, tid);
   }
@@ -225,8 +266,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int cur = (t - t0) & 1, k0 = t * KT;
     __syncthreads();                                    // tile t is staged; the other buffer is free
     if (t + 1 < t1) {
-      rk.store(sK(cur ^ 1), C::KST, k0 + KT, 0, sq.lk, tid);
-      rv.store(sV(cur ^ 1), C::VST, k0 + KT, 0, sq.lk, tid);
+      rk.store(sK(cur ^ 1), C::KST, k0 + KT, sq.lk, tid);
+      rv.store(sV(cur ^ 1), C::VST, k0 + KT, sq.lk, tid);
       rk.load(ks, k0 + 2 * KT, sq.lk, tid);
       rv.load(vs, k0 + 2 * KT, sq.lk, tid);
     }
@@ -358,21 +399,17 @@ struct WaveRows {
       x[it] = *(const V*)(p + c);
     }
   }
-  LS_DEV void store(T* lds, int ld, int row0, int hi) const {
+  LS_DEV void store(T* lds, int ld, int row0, int hi) {
     const int l = lane_id();
+    if (row0 + 32 > hi) {
+#pragma unroll
+      for (int it = 0; it < IT; ++it)
+        if (row0 + (l + 64 * it) / CPR >= hi) x[it] = V{};
+    }
 #pragma unroll
     for (int it = 0; it < IT; ++it) {
-      const int idx = l + 64 * it, r = idx / CPR, c = (idx % CPR) * VE;
-      const bool ok = row0 + r < hi;
-      V y;
-#pragma unroll
-      for (int e = 0; e < VE; ++e) y[e] = ok ? x[it][e] : (T)0.0f;
-      if ((ld * (int)sizeof(T)) % 16 == 0) {
-        *(V*)(lds + r * ld + c) = y;
-      } else {
-#pragma unroll
-        for (int e = 0; e < VE; ++e) lds[r * ld + c + e] = y[e];
-      }
+      const int idx = l + 64 * it;
+      put_piece(lds + (idx / CPR) * ld + (idx % CPR) * VE, ld, x[it]);
     }
   }
 };
@@ -504,8 +541,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct DqCfg {
-  static constexpr int KT = 32, NW = 4, NT = 64 * NW, BQ = 32 * NW;
-  static constexpr int KST = D + tr_pad<T, D>(), VST = D + MF<T>::PAD;
+  static constexpr int KT = sizeof(T) == 2 && D < 128 ? 64 : 32, NW = 4, NT = 64 * NW, BQ = 32 * NW;
+  static constexpr int KST = D + both_pad<T, D>(), VST = D + MF<T>::PAD;
   static constexpr int KB = KT * KST, VB = KT * VST;
   static constexpr int BYTES = 2 * (KB + VB) * (int)sizeof(T);
 };
@@ -563,8 +600,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   if (t0 < t1) {
     rk.load(ks, t0 * KT, sq.lk, tid);
     rv.load(vs, t0 * KT, sq.lk, tid);
-    rk.store(sK(0), C::KST, t0 * KT, 0, sq.lk, tid);
-    rv.store(sV(0), C::VST, t0 * KT, 0, sq.lk, tid);
+    rk.store(sK(0), C::KST, t0 * KT, sq.lk, tid);
+    rv.store(sV(0), C::VST, t0 * KT, sq.lk, tid);
     rk.load(ks, (t0 + 1) * KT, sq.lk, tid);
     rv.load(vs, (t0 + 1) * KT, sq.lk, tid);
   }
@@ -575,39 +612,50 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int cur = (t - t0) & 1, k0 = t * KT;
     __syncthreads();
     if (t + 1 < t1) {
-      rk.store(sK(cur ^ 1), C::KST, k0 + KT, 0, sq.lk, tid);
-      rv.store(sV(cur ^ 1), C::VST, k0 + KT, 0, sq.lk, tid);
+      rk.store(sK(cur ^ 1), C::KST, k0 + KT, sq.lk, tid);
+      rv.store(sV(cur ^ 1), C::VST, k0 + KT, sq.lk, tid);
       rk.load(ks, k0 + 2 * KT, sq.lk, tid);
       rv.load(vs, k0 + 2 * KT, sq.lk, tid);
     }
     if (qw >= sq.lq || k0 > whi || k0 + KT <= wlo) continue;
-    const T* krow = sK(cur) + col * C::KST;
-    const T* vrow = sV(cur) + col * C::VST;
-    f32x16 s = splat16(s0), dp = splat16(-delta);
+    f32x16 s[KT / 32], dp[KT / 32];
 #pragma unroll
-    for (int i = 0; i < D / F::KS; ++i) {
-      s = F::mma(F::ld(krow, i * F::KS + h * F::KPL), qf[i], s);
-      dp = F::mma(F::ld(vrow, i * F::KS + h * F::KPL), of[i], dp);
-    }
-    if (k0 < alo || k0 + KT - 1 > ahi) {
-      const int lo = live ? sq.lo(qi) : 1, hi = live ? sq.hi(qi) : 0;
+    for (int kt = 0; kt < KT / 32; ++kt) {
+      const T* krow = sK(cur) + (kt * 32 + col) * C::KST;
+      const T* vrow = sV(cur) + (kt * 32 + col) * C::VST;
+      s[kt] = splat16(s0);
+      dp[kt] = splat16(-delta);
 #pragma unroll
-      for (int v = 0; v < 16; ++v) {
-        const int j = k0 + crow(v, h);
-        const float p = fast_exp2(s[v] * a.c);
-        s[v] = j >= lo && j <= hi ? p * dp[v] : 0.0f;
+      for (int i = 0; i < D / F::KS; ++i) {
+        s[kt] = F::mma(F::ld(krow, i * F::KS + h * F::KPL), qf[i], s[kt]);
+        dp[kt] = F::mma(F::ld(vrow, i * F::KS + h * F::KPL), of[i], dp[kt]);
       }
-    } else {
+    }
+    const bool part = k0 < alo || k0 + KT - 1 > ahi;
+    const int lo = live ? sq.lo(qi) : 1, hi = live ? sq.hi(qi) : 0;
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = fast_exp2(s[v] * a.c) * dp[v];
+    for (int kt = 0; kt < KT / 32; ++kt) {
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[kt][v] = fast_exp2(s[kt][v] * a.c) * dp[kt][v];
+    }
+    if (part) {
+#pragma unroll
+      for (int kt = 0; kt < KT / 32; ++kt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int j = k0 + kt * 32 + crow(v, h);
+          s[kt][v] = j >= lo && j <= hi ? s[kt][v] : 0.0f;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < F::CSTEPS; ++i) {
-      const typename F::frag p = F::cfrag(s, i);
+    for (int kt = 0; kt < KT / 32; ++kt)
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt)
-        acc[dt] = F::mma(F::tld_crow(sK(cur), C::KST, 0, i, dt * 32), p, acc[dt]);
-    }
+      for (int i = 0; i < F::CSTEPS; ++i) {
+        const typename F::frag p = F::cfrag(s[kt], i);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          acc[dt] = F::mma(F::tld_crow(sK(cur), C::KST, kt * 32, i, dt * 32), p, acc[dt]);
+      }
   }
   if (qi >= a.nq) return;
   if (a.nsq > 1) store_col<float, D>(a.part + ((size_t)sp * a.B * a.H * a.nq + row) * D, acc, a.scale);
@@ -640,8 +688,8 @@ __global__ __launch_bounds__(256) void k_attn_sum(const float* part, T* out0, T*
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct KvCfg {
-  static constexpr int QT = 32, NW = 4, NT = 64 * NW, BK = 32 * NW;
-  static constexpr int ST = D + tr_pad<T, D>();
+  static constexpr int QT = sizeof(T) == 2 && D < 128 ? 64 : 32, NW = 4, NT = 64 * NW, BK = 32 * NW;
+  static constexpr int ST = D + both_pad<T, D>();
   static constexpr int QB = QT * ST;
   static constexpr bool VLDS = sizeof(T) == 2 && D == 128;
   static constexpr int VST = D + MF<T>::PAD;
@@ -711,8 +759,8 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     lg = wrap ? min(lg + 1, a.G - 1) : lg;
   };
   auto stage = [&](int r0, int i) {
-    rq.store(sQ(i), C::ST, r0, 0, sq.lq, tid);
-    ro.store(sO(i), C::ST, r0, 0, sq.lq, tid);
+    rq.store(sQ(i), C::ST, r0, sq.lq, tid);
+    ro.store(sO(i), C::ST, r0, sq.lq, tid);
     if (tid < 2 * QT) srow[i][tid / QT][tid & (QT - 1)] = rs;
   };
   if (total > 0) {
@@ -733,40 +781,67 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     const int re = min(rr + QT, sq.lq) - 1;
     if (jw >= sq.lk || sq.hi(re) < jw || sq.lo(rr) > jw + 31) continue;
     const bool all = rr + QT <= sq.lq && jw + 31 <= sq.hi(rr) && jw >= sq.lo(rr + QT - 1);
-    const T* qrow = sQ(cur) + col * C::ST;
-    const T* orow = sO(cur) + col * C::ST;
+    const int ilo = sq.first(kj), ihi = sq.last(kj);
     // the products start from -lse / scale and -delta of their rows
-    f32x16 s = crow_acc(srow[cur][0]);
+    f32x16 s[QT / 32], dp[QT / 32];
 #pragma unroll
-    for (int i = 0; i < D / F::KS; ++i) s = F::mma(F::ld(qrow, i * F::KS + h * F::KPL), kf[i], s);
+    for (int qt = 0; qt < QT / 32; ++qt) {
+      const T* qrow = sQ(cur) + (qt * 32 + col) * C::ST;
+      s[qt] = crow_acc(srow[cur][0] + qt * 32);
 #pragma unroll
-    for (int v = 0; v < 16; ++v) s[v] = fast_exp2(s[v] * a.c);
+      for (int i = 0; i < D / F::KS; ++i) s[qt] = F::mma(F::ld(qrow, i * F::KS + h * F::KPL), kf[i], s[qt]);
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT / 32; ++qt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) s[qt][v] = fast_exp2(s[qt][v] * a.c);
     if (!all) {
 #pragma unroll
-      for (int v = 0; v < 16; ++v) s[v] = sq.sees(rr + crow(v, h), kj) ? s[v] : 0.0f;
-    }
-    f32x16 dp = crow_acc(srow[cur][1]);
+      for (int qt = 0; qt < QT / 32; ++qt)
 #pragma unroll
-    for (int i = 0; i < D / F::KS; ++i) dp = F::mma(F::ld(orow, i * F::KS + h * F::KPL),
-                                                       C::VLDS ? F::ld(sV + (wv * 32 + col) * C::VST, i * F::KS + h * F::KPL) : vf[i], dp);
-#pragma unroll
-    for (int i = 0; i < F::CSTEPS; ++i) {
-      const typename F::frag p = F::cfrag(s, i);
-#pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) dv[dt] = F::mma(F::tld_crow(sO(cur), C::ST, 0, i, dt * 32), p, dv[dt]);
+        for (int v = 0; v < 16; ++v) {
+          const int r = rr + qt * 32 + crow(v, h);
+          s[qt][v] = r >= ilo && r <= ihi ? s[qt][v] : 0.0f;
+        }
     }
 #pragma unroll
-    for (int v = 0; v < 16; ++v) dp[v] *= s[v];
+    for (int qt = 0; qt < QT / 32; ++qt) {
+      const T* orow = sO(cur) + (qt * 32 + col) * C::ST;
+      dp[qt] = crow_acc(srow[cur][1] + qt * 32);
+#pragma unroll
+      for (int i = 0; i < D / F::KS; ++i)
+        dp[qt] = F::mma(F::ld(orow, i * F::KS + h * F::KPL),
+                        C::VLDS ? F::ld(sV + (wv * 32 + col) * C::VST, i * F::KS + h * F::KPL) : vf[i], dp[qt]);
+#pragma unroll
+      for (int i = 0; i < F::CSTEPS; ++i) {
+        const typename F::frag p = F::cfrag(s[qt], i);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          dv[dt] = F::mma(F::tld_crow(sO(cur), C::ST, qt * 32, i, dt * 32), p, dv[dt]);
+      }
+    }
+#pragma unroll
+    for (int qt = 0; qt < QT / 32; ++qt)
+#pragma unroll
+      for (int v = 0; v < 16; ++v) dp[qt][v] *= s[qt][v];
     if (!all) {                                          // (0 times whatever a key past the end holds)
 #pragma unroll
-      for (int v = 0; v < 16; ++v) dp[v] = s[v] == 0.0f ? 0.0f : dp[v];
+      for (int qt = 0; qt < QT / 32; ++qt)
+#pragma unroll
+        for (int v = 0; v < 16; ++v) {
+          const int r = rr + qt * 32 + crow(v, h);
+          dp[qt][v] = r >= ilo && r <= ihi ? dp[qt][v] : 0.0f;
+        }
     }
 #pragma unroll
-    for (int i = 0; i < F::CSTEPS; ++i) {
-      const typename F::frag ds = F::cfrag(dp, i);
+    for (int qt = 0; qt < QT / 32; ++qt)
 #pragma unroll
-      for (int dt = 0; dt < D / 32; ++dt) dk[dt] = F::mma(F::tld_crow(sQ(cur), C::ST, 0, i, dt * 32), ds, dk[dt]);
-    }
+      for (int i = 0; i < F::CSTEPS; ++i) {
+        const typename F::frag ds = F::cfrag(dp[qt], i);
+#pragma unroll
+        for (int dt = 0; dt < D / 32; ++dt)
+          dk[dt] = F::mma(F::tld_crow(sQ(cur), C::ST, qt * 32, i, dt * 32), ds, dk[dt]);
+      }
   }
   if (kj >= a.nk) return;
   int j = jw + (lane_id() & 31);
