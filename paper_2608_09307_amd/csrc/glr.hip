@@ -161,7 +161,10 @@ template <typename T, class Fn> LS_DEV typename MF<T>::frag ones_where(int L, in
 
 template <typename T> struct GlrBase {
   static constexpr int NKS = 32 / MF<T>::KS;              // k-steps over 32 rows
-  static constexpr int WST = 32 + tr_pad<T, 32>();        // row stride of a 32-channel matrix
+  // row stride of a 32-channel matrix.  Here and in the kernels' 32-row matrices 16
+  // bytes are added to a row: rows are written and read whole as often as transposed
+  // (32 heads of 16384 tokens, D = 128, backward: 517 us at tr_pad's pitch, 494 here)
+  static constexpr int WST = 32 + MF<T>::PAD;
 };
 
 // sums of this wave's 32 gates over rows picked by f(t, r): register v <-> channel 16 h + v, lane <-> t
@@ -423,7 +426,7 @@ template <typename T, int NT> LS_DEV f32x16 rows_by_rows(int h, const T* arow, c
 // ---------------------------------------------------------------------------
 template <typename T, int D> struct GlrFwd {
   static constexpr int NW = D / 32, NT = 64 * NW;
-  static constexpr int ST = D + tr_pad<T, D>(), WST = GlrBase<T>::WST;
+  static constexpr int ST = D + MF<T>::PAD, WST = GlrBase<T>::WST;
   static constexpr int NLO = sizeof(T) == 2 ? 1 : 0;
   static constexpr int MAT = 32 * ST, WM = 32 * WST;
   static constexpr int ELEMS = (4 + 2 * NLO) * MAT + 2 * NW * WM;
@@ -597,7 +600,7 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 // ---------------------------------------------------------------------------
 template <typename T, int D> struct GlrWalk {
   static constexpr int NW = D / 32, NT = 64 * NW;
-  static constexpr int ST = D + tr_pad<T, D>(), WST = GlrBase<T>::WST;
+  static constexpr int ST = D + MF<T>::PAD, WST = GlrBase<T>::WST;
   static constexpr int NLO = sizeof(T) == 2 ? 1 : 0;
   static constexpr int ELEMS = 2 * 32 * ST + (2 + NLO) * NW * 32 * WST;
 };
@@ -786,7 +789,7 @@ LS_DEV float rows_from(float x) {
 // ---------------------------------------------------------------------------
 template <typename T, int D, bool LOW> struct GlrBwd {
   static constexpr int NW = D / 32, NT = 128 * NW;
-  static constexpr int ST = D + tr_pad<T, D>(), WST = GlrBase<T>::WST, EST = 36;
+  static constexpr int ST = D + MF<T>::PAD, WST = GlrBase<T>::WST, EST = 36;
   static constexpr int MAT = 32 * ST;
   static constexpr int ELEMS = (LOW ? 10 : 8) * MAT + 2 * NW * 32 * WST;
 };
