@@ -96,6 +96,22 @@ def test_rows_that_do_not_exist_may_hold_anything(dt, D, nq, nk):
     assert not got["out"][1, :, lq[1]:].any() and not got["dk"][1, :, lk[1]:].any() and not got["dq"][2, :, 1:].any()
 
 
+@pytest.mark.parametrize("D", [32, 64, 128])
+@pytest.mark.parametrize("window", [1, 31, 32, 40, 64, 65])
+def test_mask_edges_inside_a_tile(D, window):
+    """Windows and lengths that end in either half of a tile, behind them NaN."""
+    print(f"[attn] edges {D} {window}", flush=True)
+    lq, lk = [161, 96, 33, 64], [161, 97, 65, 31]
+    x = draw(4, 2, 1, 161, 161, D, BF, seed=window)
+    ref = R.attention(*x, window=window, lens_q=lq, lens_k=lk)
+    for b in range(4):
+        for y, n in zip(x, (lq[b], lk[b], lk[b], lq[b])):
+            y[b, :, n:] = math.nan
+    got = train(*x, window=window, lens_q=lens(lq), lens_k=lens(lk))
+    for name in got:
+        R.within(got[name], ref[name], name)
+
+
 def test_later_keys_do_not_reach_earlier_rows():
     q, k, v, _ = draw(1, 2, 2, 300, 300, 64, BF, seed=5)
     a, la = L.attn_fwd(q, k, v)
