@@ -10,8 +10,8 @@
 // is formed with the contraction index of the next product on its rows, so the
 // probabilities go from accumulator registers straight into that product's
 // operand and never through LDS.  Probabilities and ds are rounded to the
-// operand type there (bf16: 2^-9 relative, random over the keys they are summed
-// over); scores, maxima, sums and outputs are float32 until the final store.
+// operand type there (bf16: 2^-8 relative at most, with errors that average out over
+// the keys they are summed over); scores, maxima, sums and outputs are float32 until the final store.
 #include "attn.h"
 
 #include <math.h>
@@ -876,7 +876,10 @@ bool attn_few(const AttnShape& s) { return s.H / s.Hkv * s.nq <= 32; }
 // partial results.  The constants are measured: a tile of 64 keys takes
 // 0.45 + 0.0075 D (float32: 0.3 + 0.05 D) on a CU, however many workgroups share
 // the CU; a round of 128 keys of the few-row kernel 0.9 + 0.005 D, and all of
-// them together the bytes of k and v at 5 TB/s.  E.g. 16 heads of 2048 tokens,
+// them together the bytes of k and v at 5 TB/s.  A workgroup that has its CU to
+// itself in the last round takes 1.36 times as long for a tile as one of two
+// (32 heads of 1000 queries, 9000 keys, D = 128: 246 us in one piece, 193 in two,
+// 219 in three, 198 in four).  E.g. 16 heads of 2048 tokens,
 // D = 128: 54 us in one piece, 46 in two; 4 heads' 64k keys for 16 heads and one
 // token: 800 us in one piece, 40 in 32 to 64.
 int attn_splits(const AttnShape& s) {
@@ -898,8 +901,10 @@ int attn_splits(const AttnShape& s) {
   double best_t = 1e300;
   for (int n = 1; n <= kMaxSplits && (n == 1 || (n * tile < most + tile && groups * n < 65536)); ++n) {
     const double longest = (most / tile / n + (few ? 1.5 : 3.0)) * us;
-    const double load = few ? groups * mean * bytes / 5e6 + groups * n * 2.0 * us / 512
-                            : groups * n * (mean / tile / n + 3.0) * us * 0.9 / 256;
+    double load = few ? groups * mean * bytes / 5e6 + groups * n * 2.0 * us / 512
+                      : groups * n * (mean / tile / n + 3.0) * us * 0.9 / 256;
+    const int fit = s.D * s.esize() >= 256 ? 2 : 3, rounds = (int)ceil(groups * n / 256);
+    if (!few && rounds > fit && rounds % fit == 1) load *= 1.0 + 0.36 / rounds;
     double t = sqrt(longest * longest + load * load);
     if (n > 1) t += 4.0 + n * partial / 4e6;
     if (t < 0.98 * best_t) { best_t = t; best = n; }
@@ -948,7 +953,7 @@ static int sweep_splits(double groups, double most, double mean, double us, doub
 
 // A tile of 32 keys takes the query sweep 0.35 + 0.0035 D us (float32: 0.4 +
 // 0.065 D), a tile of 32 queries the key sweep 0.5 + 0.0053 D (0.4 + 0.09 D).
-// 12 heads on 6 key heads, 777 tokens, D = 32, float32: key sweep 57 -> 27 us.
+// 12 heads on 6 key heads, 777 tokens, D = 32, float32: key sweep 57 -> 22 us and 6 for the sum.
 void attn_bwd_splits(const AttnShape& s, int* nsq, int* nsk) {
   const double G = (double)(s.H / s.Hkv), D = s.D;
   const bool half = s.dtype == 1;
