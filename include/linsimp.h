@@ -295,6 +295,9 @@ size_t linsimp_glr_workspace_size(const linsimp_glr_dims* dims, int for_backward
  *   S_t = diag(exp(g_t)) S_{t-1} + k_t v_t^T,   out_t = scale S_t^T q_t
  *   q, k, v, g : [B, H, n, D] dtype;  out : [B, H, n, D] dtype, written
  *   g    : logarithm of the decay, <= 0; -inf clears the channel
+ *          (values of q, k, v and dout up to 2^16 and of states up to 2^50 leave
+ *          room for factors of up to 2^60 inside a call; far larger ones can
+ *          overflow where the definition does not)
  *   s0   : [B, H, D, D] float32 state before the first row (rows: key channel),
  *          or NULL (zero);  s1 : the state after the last row, or NULL.  s1 may
  *          be s0.

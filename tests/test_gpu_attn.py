@@ -112,6 +112,20 @@ def test_mask_edges_inside_a_tile(D, window):
         R.within(got[name], ref[name], name)
 
 
+@pytest.mark.parametrize("dt,D", [(BF, 128), (BF, 32), (F32, 64)])
+@pytest.mark.parametrize("H,Hkv,nq", [(4, 2, 7), (3, 3, 31), (16, 1, 2)])
+@pytest.mark.parametrize("window", [0, 1, 33, 300])
+def test_a_few_queries(H, Hkv, nq, D, dt, window):
+    """Continuations of at most 32 rows per key head, with lengths and a scale of their own."""
+    print(f"[attn] few {H} {Hkv} {nq} {D} {dt} {window}", flush=True)
+    lq, lk = [nq, nq - 1, 1, 0], [500, 333, 2, 40]
+    x = draw(4, H, Hkv, nq, 500, D, dt, seed=window)
+    got = train(*x, window=window, scale=0.3, lens_q=lens(lq), lens_k=lens(lk))
+    ref = R.attention(*x, window=window, scale=0.3, lens_q=lq, lens_k=lk)
+    for name in got:
+        R.within(got[name], ref[name], name)
+
+
 def test_later_keys_do_not_reach_earlier_rows():
     q, k, v, _ = draw(1, 2, 2, 300, 300, 64, BF, seed=5)
     a, la = L.attn_fwd(q, k, v)

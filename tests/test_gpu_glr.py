@@ -164,6 +164,23 @@ def test_scales(scale):
         R.within(got[name], ref[name], name)
 
 
+@pytest.mark.parametrize("dt", [BF, F32])
+@pytest.mark.parametrize("mag", [1.0, 2.0 ** 15])
+@pytest.mark.parametrize("gate", [-2.55, -2.65, -30.0])
+def test_decays_at_the_limit_of_the_short_way(gate, mag, dt):
+    """16 rows of -2.55 decay by 2^58.9, of -2.65 by 2^61.2 (the limit is 2^60), with
+    values that have to fit beside such factors."""
+    print(f"[glr] limit {gate} {mag} {dt}", flush=True)
+    x = draw(2, 1, 100, 64, dt, "none", True, seed=21)
+    x["g"] += gate
+    for nm in ("q", "k", "v", "dout"):
+        x[nm] *= mag
+    got = train(x)
+    ref = R.recurrence(x["q"], x["k"], x["v"], x["g"], x["dout"], x["s0"], x["ds1"])
+    for name in got:
+        R.within(got[name], ref[name], name)
+
+
 def test_growing_gates():
     """g above zero is an ordinary exponential (the state grows)."""
     x = draw(1, 1, 64, 32, F32, "none", True, seed=5)
