@@ -74,6 +74,19 @@ template <typename T> struct Row16 {
     }
     return r;
   }
+  LS_DEV static Row16 either(bool first, const Row16& a, const Row16& b) {
+    typedef int i32x4 __attribute__((ext_vector_type(4)));
+    Row16 r;
+#pragma unroll
+    for (int i = 0; i < NV; ++i) {
+      const i32x4 x = __builtin_bit_cast(i32x4, a.p[i]), y = __builtin_bit_cast(i32x4, b.p[i]);
+      i32x4 z;
+#pragma unroll
+      for (int e = 0; e < 4; ++e) z[e] = first ? x[e] : y[e];
+      r.p[i] = __builtin_bit_cast(V, z);
+    }
+    return r;
+  }
   LS_DEV float at(int v) const { return (float)p[v / VE][v % VE]; }
   LS_DEV void set(int v, float x) { p[v / VE][v % VE] = (T)x; }
 };
@@ -187,10 +200,10 @@ struct Border {
     return (t & L) ? (r >= (t & ~(L - 1)) && r <= t ? 1.f : 0.f) : (r > t && r <= (t | (L - 1)) ? 1.f : 0.f);
   }
 };
-// pairs (s, t) that level L joins: in one block of 2 L, s in its earlier half, t in its later (L = 0: s = t)
-LS_DEV bool joins(int L, int s, int t) {
-  return L == 0 ? s == t : (t & L) != 0 && (s & L) == 0 && (t & ~(2 * L - 1)) == (s & ~(2 * L - 1));
-}
+// rows that level L joins: in the two halves of one block of 2 L (the highest bit in which they differ is L)
+LS_DEV bool joins(int L, int s, int t) { return ((s ^ t) & ~(L - 1)) == L; }
+// a row that joins none unless `ok`
+LS_DEV int row_if(bool ok, int t) { return ok ? t : t ^ 64; }
 
 // The lane, as a value of chunk c: what is derived from it (addresses, masks, the
 // matrices of ones) is then made anew in every chunk instead of being kept in
@@ -332,19 +345,15 @@ template <typename T> LS_DEV void put_decayed(int l, T* hi, T* lo, int ld, const
   put_scaled(l, hi, lo, ld, x, f, low);
 }
 
-// the rows of level L of the exact way (0: the rows as they are); returns its sums of g
+// The rows of level L of the exact way: q of the rows in later halves, k of those in
+// earlier ones, decayed from or to the border between the halves by f.  The product
+// of this matrix with itself holds the level's pairs.
 template <typename T>
-LS_DEV f32x16 put_level(int l, int L, const T* sg, T* dq, T* dk, int ld, const Row16<T>& xq, const Row16<T>& xk, float scale) {
-  const f32x16 B = gate_sum(l, sg, Border{L ? L : 32});
-  const bool later = (l & L) != 0;
-  float f[16];
+LS_DEV void put_level(int l, int L, const T* sg, T* dst, int ld, const Row16<T>& xq, const Row16<T>& xk, float (&f)[16]) {
+  const f32x16 B = gate_sum(l, sg, Border{L});
 #pragma unroll
-  for (int v = 0; v < 16; ++v) f[v] = L == 0 ? scale : later ? ex(B[v]) * scale : 0.0f;
-  put_scaled(l, dq, dq, ld, xq.again(), f, false);
-#pragma unroll
-  for (int v = 0; v < 16; ++v) f[v] = L == 0 ? 1.0f : later ? 0.0f : ex(B[v]);
-  put_scaled(l, dk, dk, ld, xk.again(), f, false);
-  return B;
+  for (int v = 0; v < 16; ++v) f[v] = ex(B[v]);
+  put_scaled(l, dst, dst, ld, Row16<T>::either((l & L) != 0, xq, xk).again(), f, false);
 }
 
 // a 32 x 32 tile as the next product's operand, all of it and with the elements (row, column) that f keeps
@@ -355,14 +364,21 @@ template <typename T> struct Tile {
 #pragma unroll
     for (int sp = 0; sp < F::CSTEPS; ++sp) f[sp] = F::cfrag(x, sp);
   }
-  template <class Fn> LS_DEV typename F::frag keep(int l, int sp, Fn fn) const {
+  // of `this` or of `other`, the rows that level L joins with the lane's column
+  LS_DEV typename F::frag level(int l, int sp, int L, const Tile& other) const {
+    const bool later = (l & L) != 0;
     if constexpr (sizeof(T) == 2) {
-      typename F::frag y;
+      typedef int i32x4 __attribute__((ext_vector_type(4)));
+      const i32x4 a = __builtin_bit_cast(i32x4, f[sp]), b = __builtin_bit_cast(i32x4, other.f[sp]);
+      i32x4 y;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) y[e] = fn(crow(8 * sp + e, l >> 5), l & 31) ? f[sp][e] : (T)0.0f;
-      return y;
+      for (int e = 0; e < 4; ++e) {
+        const bool lo = joins(L, crow(8 * sp + 2 * e, l >> 5), l & 31), hi = joins(L, crow(8 * sp + 2 * e + 1, l >> 5), l & 31);
+        y[e] = (later ? a[e] : b[e]) & ((lo ? 0xffff : 0) | (hi ? (int)0xffff0000 : 0));
+      }
+      return __builtin_bit_cast(typename F::frag, y);
     } else {
-      return fn(crow(sp, l >> 5), l & 31) ? f[sp] : 0.0f;
+      return joins(L, crow(sp, l >> 5), l & 31) ? (later ? f[sp] : other.f[sp]) : 0.0f;
     }
   }
 };
@@ -527,16 +543,27 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
       xk.load(lane_ptr((const T*)a.k + base + (size_t)32 * c * D, off));
       xq.keep(ok); xk.keep(ok);
       gate_exact(l, sg);
-#pragma unroll 1
-      for (int L = 0; L <= 16; L = L ? 2 * L : 1) {
-        __syncthreads();
-        put_level(l, L, sg, sQ(i) + 32 * w, sK(i) + 32 * w, ST, xq, xk, a.scale);
-        __syncthreads();
-        const f32x16 M = rows_by_rows<T, NW>(h, krow, qrow);
+      put_row(sQ(i) + col * ST + 32 * w + 16 * h, xq);
+      put_row(sK(i) + col * ST + 32 * w + 16 * h, xk);
+      __syncthreads();
+      f32x16 M = rows_by_rows<T, NW>(h, krow, qrow);
 #pragma unroll
-        for (int v = 0; v < 16; ++v) P[v] = joins(L, crow(v, h), col) ? M[v] : P[v];
-      }
+      for (int v = 0; v < 16; ++v) P[v] = crow(v, h) == col ? M[v] : P[v];
+      __syncthreads();
       float f[16];
+      bool odd = true;                               // (two matrices in turn: one barrier for a level)
+#pragma unroll 1
+      for (int L = 1; L <= 16; L *= 2, odd = !odd) {
+        T* X = odd ? sK(i) : sQ(i);
+        put_level(l, L, sg, X + 32 * w, ST, xq, xk, f);
+        __syncthreads();
+        M = rows_by_rows<T, NW>(h, X + col * ST, X + col * ST);
+        const int tc = row_if((col & L) != 0, col);
+#pragma unroll
+        for (int v = 0; v < 16; ++v) P[v] = joins(L, crow(v, h), tc) ? M[v] : P[v];
+      }
+#pragma unroll
+      for (int v = 0; v < 16; ++v) P[v] *= a.scale;
       __syncthreads();
       border_exact(l, sg, slo + 32 * w, spend[i] + 32 * w, spend[i ^ 1] + 32 * w, sfz[i] + 32 * w, sall + 32 * w);
       f32x16 B = gate_sum(l, sg, UpTo{});
@@ -1034,26 +1061,29 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
         keep_pairs(rows_by_rows<T, NW>(h, vrow, orow), rows_by_rows<T, NW>(h, orow, vrow));
 #pragma unroll
         for (int v = 0; v < 16; ++v) dq[v] = dk[v] = x[v] = 0.0f;
+        put_row(qme, xq);                                // (the diagonal, for the value waves)
+        put_row(kme, xk);
+        __syncthreads();
+        __syncthreads();
+        bool odd = true;                                 // (two matrices in turn: one barrier for a level)
 #pragma unroll 1
-        for (int L = 0; L <= 16; L = L ? 2 * L : 1) {            // (L = 0, the diagonal: for the value waves)
+        for (int L = 1; L <= 16; L *= 2, odd = !odd) {
+          T* X = odd ? sK(i) : sQ(i);
+          float f[16], y[16];
+          put_level(l, L, sg, X + 32 * w, ST, xq, xk, f);
           __syncthreads();
-          const f32x16 B = put_level(l, L, sg, sQ(i) + 32 * w, sK(i) + 32 * w, ST, xq, xk, a.scale);
-          __syncthreads();
-          f32x16 bq = zero16(), bk = zero16();
+          f32x16 b = zero16();
 #pragma unroll
-          for (int sp = 0; sp < F::CSTEPS; ++sp) {
-            bq = F::mma(rows_crow<true>(l, sK(i), ST, sp, 32 * w),
-                        dPt.keep(l, sp, [L](int s, int t_) { return L != 0 && joins(L, s, t_); }), bq);
-            bk = F::mma(rows_crow<true>(l, sQ(i), ST, sp, 32 * w),
-                        dP.keep(l, sp, [L](int t_, int s) { return L != 0 && joins(L, s, t_); }), bk);
+          for (int sp = 0; sp < F::CSTEPS; ++sp) b = F::mma(rows_crow<true>(l, X, ST, sp, 32 * w), dPt.level(l, sp, L, dP), b);
+          get_row(X + col * ST + 32 * w + 16 * h, y);
+          const bool later = (col & L) != 0;             // b is of dq in later halves, of dk in earlier ones
+#pragma unroll
+          for (int v = 0; v < 16; ++v) {
+            const float z = b[v] * a.scale, e = f[v] * z;
+            x[v] = __builtin_fmaf(later ? y[v] : -y[v], z, x[v]);
+            dq[v] += later ? e : 0.0f;
+            dk[v] += later ? 0.0f : e;
           }
-          float y[16];
-          get_row(qme, y);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) { x[v] += y[v] * bq[v]; dq[v] += ((col & L) ? ex(B[v]) * a.scale : 0.0f) * bq[v]; }
-          get_row(kme, y);
-#pragma unroll
-          for (int v = 0; v < 16; ++v) { x[v] -= y[v] * bk[v]; dk[v] += ((col & L) ? 0.0f : ex(B[v])) * bk[v]; }
         }
         {
           float f[16];
@@ -1168,14 +1198,23 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 #pragma unroll
         for (int v = 0; v < 16; ++v) P[v] = crow(v, h) >= col ? P[v] : 0.0f;
       } else {
-#pragma unroll 1
-        for (int L = 0; L <= 16; L = L ? 2 * L : 1) {
-          __syncthreads();
-          __syncthreads();
-          const f32x16 M = rows_by_rows<T, NW>(h, qrow, krow);
+        __syncthreads();
+        f32x16 M = rows_by_rows<T, NW>(h, qrow, krow);
 #pragma unroll
-          for (int v = 0; v < 16; ++v) P[v] = joins(L, col, crow(v, h)) ? M[v] : P[v];
+        for (int v = 0; v < 16; ++v) P[v] = crow(v, h) == col ? M[v] : P[v];
+        __syncthreads();
+        bool odd = true;
+#pragma unroll 1
+        for (int L = 1; L <= 16; L *= 2, odd = !odd) {
+          const T* X = (odd ? sK(i) : sQ(i)) + col * ST;
+          __syncthreads();
+          M = rows_by_rows<T, NW>(h, X, X);
+          const int sc = row_if((col & L) == 0, col);
+#pragma unroll
+          for (int v = 0; v < 16; ++v) P[v] = joins(L, sc, crow(v, h)) ? M[v] : P[v];
         }
+#pragma unroll
+        for (int v = 0; v < 16; ++v) P[v] *= a.scale;
         __syncthreads();
         __syncthreads();
         scale_rows<NW>(l, R, sfz[i]);
