@@ -1099,6 +1099,10 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
           put_scaled(l, sK(i) + 32 * w, sK(i), ST, xk.again(), f, false);
           __syncthreads();
         }
+#pragma unroll
+        for (int et = 0; et < NW; ++et)                  // (read again, rather than kept through the levels)
+#pragma unroll
+          for (int sp = 0; sp < F::CSTEPS; ++sp) z[et][sp] = zs[(et * F::CSTEPS + sp) * 64];
         outside(sfz[i][me], std::integral_constant<bool, false>{});
         through *= sall[me];
         put_w();
