@@ -197,7 +197,9 @@ struct All { LS_DEV float operator()(int, int) const { return 1.f; } };
 struct Border {
   int L;
   LS_DEV float operator()(int t, int r) const {
-    return (t & L) ? (r >= (t & ~(L - 1)) && r <= t ? 1.f : 0.f) : (r > t && r <= (t | (L - 1)) ? 1.f : 0.f);
+    const bool later = (t & L) != 0;
+    const int from = later ? t & ~(L - 1) : t + 1, rows = later ? t - from + 1 : (t | (L - 1)) - t;
+    return (unsigned)(r - from) < (unsigned)rows ? 1.f : 0.f;
   }
 };
 // rows that level L joins: in the two halves of one block of 2 L (the highest bit in which they differ is L)
@@ -1099,6 +1101,7 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
           put_scaled(l, sK(i) + 32 * w, sK(i), ST, xk.again(), f, false);
           __syncthreads();
         }
+        __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
         for (int et = 0; et < NW; ++et)                  // (read again, rather than kept through the levels)
 #pragma unroll
@@ -1116,12 +1119,14 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 #pragma unroll
         for (int v = 0; v < 16; ++v) { x[v] -= y[v] * ak[v]; dk[v] += ex(B[v]) * ak[v]; }
         put_dg(x);
-        const Row16<T> yq = xq.again(), yk = xk.again();
+        __builtin_amdgcn_sched_barrier(0);
+        rows_of(xq, xk);                                 // (again)
+        xq.keep(ok); xk.keep(ok);
         diag *= a.scale;
 #pragma unroll
         for (int v = 0; v < 16; ++v) {
-          dq[v] = __builtin_fmaf(diag, yk.at(v), dq[v]);
-          dk[v] = __builtin_fmaf(diag, yq.at(v), dk[v]);
+          dq[v] = __builtin_fmaf(diag, xk.at(v), dq[v]);
+          dk[v] = __builtin_fmaf(diag, xq.at(v), dk[v]);
         }
         put_grad(a.dq, dq);
         put_grad(a.dk, dk);
