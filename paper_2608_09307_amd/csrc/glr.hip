@@ -349,7 +349,9 @@ template <typename T> LS_DEV void put_decayed(int l, T* hi, T* lo, int ld, const
 
 // The rows of level L of the exact way: q of the rows in later halves, k of those in
 // earlier ones, decayed from or to the border between the halves by f.  The product
-// of this matrix with itself holds the level's pairs.
+// of this matrix with itself holds the level's pairs (against a matrix of each, with
+// half of the rows zero: 48 heads of 2048 tokens, D = 64, resets in every chunk,
+// forward and backward 364 -> 266 us).
 template <typename T>
 LS_DEV void put_level(int l, int L, const T* sg, T* dst, int ld, const Row16<T>& xq, const Row16<T>& xk, float (&f)[16]) {
   const f32x16 B = gate_sum(l, sg, Border{L});
