@@ -38,8 +38,8 @@ FLAGS = [
 # spilled 60 instead of 75 registers at its 256 and ran 3-4% faster (today's
 # spills 24 at d = m = 128 with it and without; elsewhere the option raised
 # register counts and lowered occupancy, so it stays local).  Attention's key
-# sweep at d = 128 spills none of its 256 registers with it instead of four:
-# 16 heads of 16384 tokens 2.39 -> 2.29 ms.
+# sweep at d = 128 spills no register with it instead of eight: 16 heads of
+# 16384 tokens 2.27 -> 2.08 ms.
 SOURCE_FLAGS = {"bwd.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"],
                 "attn.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"]}
 
