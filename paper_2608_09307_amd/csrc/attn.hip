@@ -224,16 +224,6 @@ struct FwdCfg {
   static constexpr int BYTES = 2 * (KB + VB) * (int)sizeof(T);
 };
 
-// Products before the exps of the SIMD's other wave, at D = 128 (32 heads of 1000
-// queries against 9000 keys: 187 -> 176 us; 16 heads of 16384 causal tokens: the
-// same; 48 heads of 2048 at D = 64, where exps are as much work, 51 -> 53).
-template <int D> LS_DEV void products_first(int on) {
-  if constexpr (D == 128) {
-    if (on) __builtin_amdgcn_s_setprio(1);
-    else __builtin_amdgcn_s_setprio(0);
-  }
-}
-
 template <typename T, int D>
 __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k_attn_fwd(AttnArgs a) {
   using F = MF<T>;
@@ -289,7 +279,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
     }
     if (qw >= sq.lq || k0 > whi || k0 + KT <= wlo) continue;
     f32x16 s[KT / 32];
-    products_first<D>(1);
 #pragma unroll
     for (int kt = 0; kt < KT / 32; ++kt) {
       const T* krow = sK(cur) + (kt * 32 + col) * C::KST;
@@ -297,7 +286,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 #pragma unroll
       for (int i = 0; i < D / F::KS; ++i) s[kt] = F::mma(F::ld(krow, i * F::KS + h * F::KPL), qf[i], s[kt]);
     }
-    products_first<D>(0);
     if (k0 < alo || k0 + KT - 1 > ahi) {
       const int lo = sq.lo(qi), hi = sq.hi(qi);
 #pragma unroll
@@ -309,7 +297,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         }
     }
     st.absorb(s, a.c);
-    products_first<D>(1);
 #pragma unroll
     for (int kt = 0; kt < KT / 32; ++kt)
 #pragma unroll
@@ -319,7 +306,6 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
         for (int et = 0; et < D / 32; ++et)
           st.o[et] = F::mma(F::tld_crow(sV(cur), C::VST, kt * 32, i, et * 32), p, st.o[et]);
       }
-    products_first<D>(0);
   }
   const float lt = half_swap_add(st.l);
   if (qi >= a.nq) return;
