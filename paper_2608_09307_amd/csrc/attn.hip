@@ -883,7 +883,9 @@ static int launch_status(const char* what) {
   return -4;
 }
 
-bool attn_few(const AttnShape& s) { return s.H / s.Hkv * s.nq <= 32; }
+// Whether the few-row kernel runs, and so which time model the splits come from:
+// single tokens always (the step has no other kernel).
+bool attn_few(const AttnShape& s) { return s.nq == 1 || s.H / s.Hkv * s.nq <= 32; }
 
 // Workgroups that share one query tile's (or key head's) keys, from the time in
 // microseconds: the longest workgroup's key tiles and the whole load at the rate
@@ -897,7 +899,9 @@ bool attn_few(const AttnShape& s) { return s.H / s.Hkv * s.nq <= 32; }
 // (32 heads of 1000 queries, 9000 keys, D = 128: 246 us in one piece, 193 in two,
 // 219 in three, 198 in four).  E.g. 16 heads of 2048 tokens,
 // D = 128: 54 us in one piece, 46 in two; 4 heads' 64k keys for 16 heads and one
-// token: 800 us in one piece, 40 in 32 to 64.
+// token: 800 us in one piece, 40 in 32 to 64.  A step of 4 sequences, 64 heads on
+// one key head, 64k slots, D = 128: 157 us in 4 pieces, 43 in the 38 taken; 8
+// sequences, 128 heads on one, 32k slots: 297 in one piece, 49 in 16.
 int attn_splits(const AttnShape& s) {
   const bool few = attn_few(s);
   const int64_t ntq = few ? 1 : (s.nq + 127) / 128;
@@ -932,7 +936,7 @@ template <typename T, int D>
 static int run_fwd(const AttnShape& s, AttnArgs a, hipStream_t st) {
   const char* what = a.pos != nullptr ? "attn step" : "attn forward";
   (void)hipGetLastError();
-  if (a.pos != nullptr || attn_few(s)) {
+  if (attn_few(s)) {
     const dim3 grid((unsigned)(s.B * s.Hkv * a.ns), (unsigned)((a.G * a.nq + 31) / 32));
     ProfScope ps(a.pos != nullptr ? "attn_step" : "attn_few", st);
     if (a.pos != nullptr) k_attn_few<T, D, true><<<grid, 256, 0, st>>>(a);

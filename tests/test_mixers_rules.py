@@ -1,0 +1,26 @@
+"""Which kernel, how many pieces: the rules of the mixers' host side, as far as the
+workspace's size shows them (no GPU needed)."""
+
+import pytest
+
+from paper_2608_09307_amd import linsimp as L
+
+
+def pieces(d):
+    """Pieces that the keys of a forward or a step are split into: each writes a row
+    of D values, a maximum and a sum for every query (256-byte steps, two arrays)."""
+    rows = d.B * d.H * d.nq
+    size = L.attn_workspace_size(d, False)
+    al = lambda x: -(-x // 256) * 256  # noqa: E731
+    n = [n for n in range(2, 65) if al(n * rows * d.D * 4) + al(n * rows * 8) == size]
+    return n[0] if n else 1
+
+
+@pytest.mark.parametrize("B,H,Hkv,cap,D", [(8, 128, 1, 32768, 128), (16, 128, 1, 8192, 128), (1, 128, 1, 65536, 128),
+                                          (4, 64, 1, 65536, 128), (4, 64, 8, 65536, 128), (1, 40, 1, 65536, 32)])
+def test_a_step_of_few_heads_over_long_rings_fills_the_chip(B, H, Hkv, cap, D):
+    """A workgroup of the step takes 32 heads of one key head: the pieces of the ring
+    have to make up for the few of them, however many heads share a key head."""
+    n = pieces(L.AttnDims(B, H, Hkv, 1, cap, 0, D, L.BF16, 1, 0.1))
+    groups = B * Hkv * -(-(H // Hkv) // 32)
+    assert groups * n >= 128, (groups, n)
