@@ -374,8 +374,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 
 // ---------------------------------------------------------------------------
 // Few queries over a long axis (the single-token step, and forwards of at most
-// 32 queries per key head).  The queries of all heads that share a key head are
-// the columns of one tile, so the keys are read once for all of them.  Each wave
+// 32 queries per head).  The queries of all heads that share a key head are the
+// columns of a tile, so the keys are read once for 32 of them.  Each wave
 // walks keys of its own in tiles of 32, through LDS of its own, without a
 // barrier until the four waves (and then the ns workgroups) are joined.  Bound
 // by the cache's bytes: one tile is in LDS and the next in flight in registers.
@@ -883,9 +883,16 @@ static int launch_status(const char* what) {
   return -4;
 }
 
-// Whether the few-row kernel runs, and so which time model the splits come from:
-// single tokens always (the step has no other kernel).
-bool attn_few(const AttnShape& s) { return s.nq == 1 || s.H / s.Hkv * s.nq <= 32; }
+// Whether the few-row kernel runs (the step has no other), and so which time model
+// the splits come from.  It reads a key head's keys once per 32 columns, the tiled
+// kernel once per head and 128 queries: up to 32 queries of a head never more often.
+// Microseconds, tiled / few-row, at G heads on a key head:
+//   64 sequences, 4 key heads, G = 4, 2048 keys, D = 128:  nq = 12: 153/81, 24: 152/121,
+//     32: 152/156, 48: 154/234;  D = 64: 94/28, 94/48, 94/69, 98/102
+//   4 sequences, 2 key heads, G = 8, 65536 keys, D = 128:  nq = 6: 318/76, 32: 320/150
+//   16 sequences, 8 heads, G = 1, 4096 keys, D = 128:  nq = 32: 52/48, 48: 52/43, 96: 67/109
+// (the last condition: column groups are the grid's second dimension)
+bool attn_few(const AttnShape& s) { return s.nq <= 32 && s.H / s.Hkv * s.nq <= 32 * 65535; }
 
 // Workgroups that share one query tile's (or key head's) keys, from the time in
 // microseconds: the longest workgroup's key tiles and the whole load at the rate
