@@ -1361,25 +1361,34 @@ template <typename T, int D> static int run_fwd(const GlrShape& s, const GlrArgs
   (void)hipGetLastError();
   if (a.G > 1)
     if (int rc = run_parts<T, D, false>(s, a, st)) return rc;
-  ProfScope ps("glr_fwd", st);
-  k_glr_fwd<T, D, false><<<(unsigned)(s.BH() * a.G), 2 * D, 0, st>>>(a);
-  k_glr_fwd<T, D, true><<<(unsigned)(s.BH() * a.G), 2 * D, 0, st>>>(a);
-  return launch_status("glr forward");
+  const unsigned grid = (unsigned)(s.BH() * a.G);
+  {
+    ProfScope ps("glr_fwd", st);
+    k_glr_fwd<T, D, false><<<grid, 2 * D, 0, st>>>(a);
+  }
+  if (int rc = launch_status("glr forward")) return rc;
+  ProfScope ps("glr_fwd_exact", st);
+  k_glr_fwd<T, D, true><<<grid, 2 * D, 0, st>>>(a);
+  return launch_status("glr forward, exact way");
+}
+
+// the short way's launch, then that of the segments that it left
+template <typename T, int D, bool LOW> static int run_sweeps(const GlrShape& s, const GlrArgs& a, hipStream_t st) {
+  const unsigned grid = (unsigned)(s.BH() * a.G);
+  {
+    ProfScope ps("glr_bwd", st);
+    k_glr_bwd<T, D, false, LOW><<<grid, 4 * D, 0, st>>>(a);
+  }
+  if (int rc = launch_status("glr backward")) return rc;
+  ProfScope ps("glr_bwd_exact", st);
+  k_glr_bwd<T, D, true, LOW><<<grid, 4 * D, 0, st>>>(a);
+  return launch_status("glr backward, exact way");
 }
 
 template <typename T, int D> static int run_bwd(const GlrShape& s, const GlrArgs& a, hipStream_t st) {
   (void)hipGetLastError();
   if (int rc = run_parts<T, D, true>(s, a, st)) return rc;
-  ProfScope ps("glr_bwd", st);
-  const unsigned grid = (unsigned)(s.BH() * a.G);
-  if (sizeof(T) == 2 && a.exact) {
-    k_glr_bwd<T, D, false, sizeof(T) == 2><<<grid, 4 * D, 0, st>>>(a);
-    k_glr_bwd<T, D, true, sizeof(T) == 2><<<grid, 4 * D, 0, st>>>(a);
-  } else {
-    k_glr_bwd<T, D, false, false><<<grid, 4 * D, 0, st>>>(a);
-    k_glr_bwd<T, D, true, false><<<grid, 4 * D, 0, st>>>(a);
-  }
-  return launch_status("glr backward");
+  return sizeof(T) == 2 && a.exact ? run_sweeps<T, D, sizeof(T) == 2>(s, a, st) : run_sweeps<T, D, false>(s, a, st);
 }
 
 #define GLR_DISPATCH(FN, ...)                                                    \
