@@ -903,8 +903,10 @@ bool attn_few(const AttnShape& s) { return s.nq <= 32 && s.H / s.Hkv * s.nq <= 3
 // the CU; a round of 128 keys of the few-row kernel 0.9 + 0.005 D, and all of
 // them together the bytes of k and v at 5 TB/s.  A workgroup that has its CU to
 // itself in the last round takes 1.36 times as long for a tile as one of two
-// (32 heads of 1000 queries, 9000 keys, D = 128: 246 us in one piece, 193 in two,
-// 219 in three, 198 in four).  E.g. 16 heads of 2048 tokens,
+// (32 heads of 1000 queries, 9000 keys, D = 128, where two fit: 246 us in one
+// piece, 193 in two, 219 in three, 198 in four; D = 64, three: 99 in two, 102 in
+// three, 112 in four, 107 in eight; D = 32, five: 74 in three, 70 in four, 76 in
+// six; 64 heads, D = 32: 136 in two, 139 in three).  E.g. 16 heads of 2048 tokens,
 // D = 128: 54 us in one piece, 46 in two; 4 heads' 64k keys for 16 heads and one
 // token: 800 us in one piece, 40 in 32 to 64.  A step of 4 sequences, 64 heads on
 // one key head, 64k slots, D = 128: 157 us in 4 pieces, 43 in the 38 taken; 8
@@ -922,6 +924,8 @@ int attn_splits(const AttnShape& s) {
   }
   const double tile = few ? 128.0 : 64.0;
   const double us = few ? 0.9 + 0.005 * s.D : s.dtype == 1 ? 0.45 + 0.0075 * s.D : 0.3 + 0.05 * s.D;
+  // workgroups of the tiled kernel that a CU holds (registers at D = 32, LDS above)
+  const int fit = s.D == 32 ? (s.dtype == 1 ? 5 : 4) : s.D * s.esize() >= 256 ? 2 : 3;
   const double bytes = 2.0 * s.D * (double)s.esize();     // of one key and value
   const double partial = (double)(s.B * s.H * s.nq) * (s.D + 2) * 4.0;
   int best = 1;
@@ -930,7 +934,7 @@ int attn_splits(const AttnShape& s) {
     const double longest = (most / tile / n + (few ? 1.5 : 3.0)) * us;
     double load = few ? groups * mean * bytes / 5e6 + groups * n * 2.0 * us / 512
                       : groups * n * (mean / tile / n + 3.0) * us * 0.9 / 256;
-    const int fit = s.D * s.esize() >= 256 ? 2 : 3, rounds = (int)ceil(groups * n / 256);
+    const int rounds = (int)ceil(groups * n / 256);
     if (!few && rounds > fit && rounds % fit == 1) load *= 1.0 + 0.36 / rounds;
     double t = sqrt(longest * longest + load * load);
     if (n > 1) t += 4.0 + n * partial / 4e6;

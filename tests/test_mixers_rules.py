@@ -24,3 +24,11 @@ def test_a_step_of_few_heads_over_long_rings_fills_the_chip(B, H, Hkv, cap, D):
     n = pieces(L.AttnDims(B, H, Hkv, 1, cap, 0, D, L.BF16, 1, 0.1))
     groups = B * Hkv * -(-(H // Hkv) // 32)
     assert groups * n >= 128, (groups, n)
+
+
+def test_a_lone_workgroup_in_the_last_round_is_one_past_what_a_cu_holds():
+    """D = 32: a CU holds five workgroups (float32: four), not three: 64 heads of 1000
+    queries against 9000 keys take two pieces (136 us in two, 139 in three)."""
+    for dt in (L.BF16, L.F32):
+        assert pieces(L.AttnDims(4, 16, 4, 1000, 9000, 0, 32, dt, 1, 0.1)) == 2
+    assert pieces(L.AttnDims(2, 16, 4, 1000, 9000, 0, 128, L.BF16, 1, 0.1)) == 2
