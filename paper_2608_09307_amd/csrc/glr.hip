@@ -1319,17 +1319,30 @@ static int launch_status(const char* what) {
   return -4;
 }
 
+// Workgroups of the main kernel that a CU is counted with.  LDS lets it hold, forward
+// at D = 32, 64, 128: 7, 4, 2 (float32 6, 3), backward: 4, 2, 1 (float32 3, 1), and these
+// are taken except at two places in float32, where the measurements are against them.
+// Microseconds of 32 heads of 16384, 256 of 1024 and 32 of 4096 tokens:
+//   forward D = 32 bf16, counted 4: 66, 38, 28, 7: 61, 36, 29;  float32, 4: 130, 69, 45,
+//   6: 143, 81, 53;  forward D = 64 float32, 4: 409, 191, 107, 3: 359, 183, 111;
+//   backward D = 32 float32, 4: 376, 190, 103, 3: 339, 167, 97;  backward D = 64 float32,
+//   2: 914, 450, 248, 1: 1000, 450, 265
+static int counted_per_cu(const GlrShape& s, bool backward) {
+  const bool half = s.dtype == 1;
+  if (backward) return s.D == 128 ? 1 : s.D == 64 ? 2 : half ? 4 : 3;
+  return s.D == 128 ? 2 : s.D == 64 ? (half ? 4 : 3) : half ? 7 : 4;
+}
+
 // Segments per (sequence, head): the count that minimises the time in units of
-// one chunk of the main kernel, `slots` workgroups running at once: rounds times
-// (chunks per segment + its prologue and stores), and for more than one segment
+// one chunk of the main kernel, `slots` workgroups counted as running at once: rounds
+// times (chunks per segment + its prologue and stores), and for more than one segment
 // the walk that finds the segments' parts, the scan and two launches.  Forward
 // and backward, D = 64, 48 heads of 2048 tokens: 427 us in one segment, 177 in 4,
 // 137 in 8, 124 in 16, 151 in 32 (this rule: 16 forward, 10 backward, 121 us);
 // D = 128, 32 heads of 16384: 5.7 ms in one, 1.84 in 4, 1.12 in 8 or 16, 1.38 in
 // 64 (16 forward, 8 backward, 1.07 ms).
 int glr_segments(const GlrShape& s, bool backward) {
-  const int64_t per_cu = backward ? (s.D == 128 ? 1 : s.D == 64 ? 2 : 4) : (s.D == 128 ? 2 : 4);
-  const int64_t slots = 256 * per_cu, BH = s.BH(), nch = s.nch();
+  const int64_t slots = 256 * (int64_t)counted_per_cu(s, backward), BH = s.BH(), nch = s.nch();
   const double kEnds = 2.0, kWalk = backward ? 0.7 : 0.6, kLaunch = backward ? 4.0 : 6.0;
   int best = 1;
   double best_t = 1e300;

@@ -31,3 +31,22 @@ def test_a_lone_workgroup_in_the_last_round_is_one_past_what_a_cu_holds():
     queries against 9000 keys take two pieces (136 us in two, 139 in three)."""
     for dt in (L.BF16, L.F32):
         assert pieces(L.AttnDims(4, 16, 4, 1000, 9000, 0, 32, dt, 1, 0.1)) == 2
+
+
+def segments(d):
+    """Segments of a forward of the recurrence: a word, and where there is more than one
+    a state and a decay of each (256-byte steps)."""
+    al = lambda x: -(-x // 256) * 256  # noqa: E731
+    size, bh = L.glr_workspace_size(d, False), d.B * d.H
+    n = [n for n in range(2, 257) if al(bh * n * 4) + al(bh * n * d.D * d.D * 4) + al(bh * n * d.D * 4) == size]
+    return n[0] if n else 1
+
+
+@pytest.mark.parametrize("D,dt,fits", [(32, L.BF16, 7), (64, L.BF16, 4), (128, L.BF16, 2), (64, L.F32, 3)])
+@pytest.mark.parametrize("B,H,n", [(2, 16, 16384), (1, 8, 16384)])
+def test_segments_fill_one_round_of_what_a_cu_holds(B, H, n, D, dt, fits):
+    """Long sequences of a few heads: the shortest segments, in whole chunks of 32 rows,
+    that run at once."""
+    g, chunks = segments(L.GlrDims(B, H, n, D, dt, 0.1)), n // 32
+    per = -(-chunks // g)
+    assert B * H * g <= 256 * fits < B * H * -(-chunks // (per - 1)), (g, per)
