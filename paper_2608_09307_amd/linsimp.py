@@ -530,10 +530,10 @@ def glr_workspace_size(d: GlrDims, backward: bool) -> int:
 
 def _mixer_workspace(workspace, nbytes, device):
     """The caller's workspace (the library checks its size, and the dims), or a new
-    one of ``nbytes``, which only then has to be known."""
-    if nbytes == 0:
-        _check(-2)                                     # the message of the refused dims
+    one of ``nbytes`` (None beside a caller's: the size costs a call)."""
     if workspace is None:
+        if nbytes == 0:
+            _check(-2)                                 # the message of the refused dims
         return alloc_bytes(nbytes, device)
     if workspace.get_device() != device.index:
         raise ValueError(f"workspace is on {workspace.device}, expected {device}")
@@ -569,7 +569,8 @@ def attn_fwd(q, k, v, causal=True, window=0, scale=None, lens_q=None, lens_k=Non
     ptrs, (pq, pk, pl) = _with_optional(
         _attn_inputs(q, k, v, d) + [(out, "out", q.shape, q.dtype)],
         _attn_lens(lens_q, lens_k, d.B) + [(lse, "lse", q.shape[:3], torch.float32)])
-    workspace = _mixer_workspace(workspace, workspace is not None or attn_workspace_size(d, False), q.device)
+    nbytes = attn_workspace_size(d, False) if workspace is None else None
+    workspace = _mixer_workspace(workspace, nbytes, q.device)
     _check(lib().linsimp_attn_fwd(ctypes.byref(d), *ptrs[:3], pq, pk, ptrs[3], pl, _ptr(workspace, "workspace"),
                                   workspace.numel(), _stream()))
     return out, lse
@@ -587,7 +588,8 @@ def attn_bwd(q, k, v, out, lse, dout, causal=True, window=0, scale=None, lens_q=
         + [(out, "out", q.shape, q.dtype), (lse, "lse", q.shape[:3], torch.float32), (dout, "dout", q.shape, q.dtype)]
         + [(g, "d" + nm, x.shape, x.dtype) for g, nm, x in zip(grads, "qkv", (q, k, v))],
         _attn_lens(lens_q, lens_k, d.B))
-    workspace = _mixer_workspace(workspace, workspace is not None or attn_workspace_size(d, True), q.device)
+    nbytes = attn_workspace_size(d, True) if workspace is None else None
+    workspace = _mixer_workspace(workspace, nbytes, q.device)
     _check(lib().linsimp_attn_bwd(ctypes.byref(d), *ptrs[:3], pq, pk, *ptrs[3:], _ptr(workspace, "workspace"),
                                   workspace.numel(), _stream()))
     return tuple(grads)
@@ -608,7 +610,8 @@ def attn_step(kcache, vcache, pos, q, k, v, scale=None, out=None, workspace=None
     ptrs = _expect([(q, "q", (B, H, D), dt), (k, "k", (B, Hkv, D), dt), (v, "v", (B, Hkv, D), dt),
                     (kcache, "kcache", (B, Hkv, cap, D), dt), (vcache, "vcache", (B, Hkv, cap, D), dt),
                     (pos, "pos", (B,), torch.int64), (out, "out", (B, H, D), dt)])
-    workspace = _mixer_workspace(workspace, workspace is not None or attn_workspace_size(d, False), q.device)
+    nbytes = attn_workspace_size(d, False) if workspace is None else None
+    workspace = _mixer_workspace(workspace, nbytes, q.device)
     _check(lib().linsimp_attn_step(ctypes.byref(d), *ptrs, _ptr(workspace, "workspace"), workspace.numel(),
                                    _stream()))
     return out
@@ -633,7 +636,8 @@ def glr_fwd(q, k, v, g, s0=None, lens=None, scale=None, out=None, s1=None, want_
     ptrs, (p0, pl, p1) = _with_optional(
         _glr_inputs(q, k, v, g) + [(out, "out", q.shape, q.dtype)],
         [(s0, "s0", st, torch.float32), (lens, "lens", (d.B,), torch.int32), (s1, "s1", st, torch.float32)])
-    workspace = _mixer_workspace(workspace, workspace is not None or glr_workspace_size(d, False), q.device)
+    nbytes = glr_workspace_size(d, False) if workspace is None else None
+    workspace = _mixer_workspace(workspace, nbytes, q.device)
     _check(lib().linsimp_glr_fwd(ctypes.byref(d), *ptrs[:4], p0, pl, ptrs[4], p1, _ptr(workspace, "workspace"),
                                  workspace.numel(), _stream()))
     return out, s1
@@ -656,7 +660,8 @@ def glr_bwd(q, k, v, g, dout, s0=None, lens=None, ds1=None, scale=None, grads=No
         + [(x, "d" + nm, q.shape, q.dtype) for x, nm in zip(grads, "qkvg")],
         [(s0, "s0", st, torch.float32), (lens, "lens", (d.B,), torch.int32), (ds1, "ds1", st, torch.float32),
          (ds0, "ds0", st, torch.float32)])
-    workspace = _mixer_workspace(workspace, workspace is not None or glr_workspace_size(d, True), q.device)
+    nbytes = glr_workspace_size(d, True) if workspace is None else None
+    workspace = _mixer_workspace(workspace, nbytes, q.device)
     _check(lib().linsimp_glr_bwd(ctypes.byref(d), *ptrs[:4], p0, pl, ptrs[4], p1, *ptrs[5:], pd,
                                  _ptr(workspace, "workspace"), workspace.numel(), _stream()))
     return (*grads, ds0)
