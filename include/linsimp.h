@@ -206,17 +206,29 @@ int linsimp_decode_chunk(int64_t S, int32_t H, int32_t T, int32_t D, int32_t Dv,
                          float* a, float* rho, void* ring_r, void* ring_u, int64_t* pos, void* out,
                          void* stream);
 
-/* ---- The mixers that a LinSimp stack interleaves with ----
+/* ---- Two mixers beside LinSimp ----
  *
- * Softmax attention and the gated linear recurrence (the layers between the
- * LinSimp layers of the paper's hybrid models, Sec. 4), behind the conventions
- * above: dense [B, heads, rows, D] device tensors, 16-byte aligned, the
- * caller's workspace (256-byte aligned), calls that only enqueue on `stream`,
- * negative statuses.  D is 32, 64 or 128 with LINSIMP_BF16 and 32 or 64 with
- * LINSIMP_F32.  Results are the same bits on every run of a call.  Sizes:
- * attention B*H <= 2^20, B*H*nq <= 2^30, nk <= 2^30, and for the backward
- * B*Hkv*nk <= 2^30; recurrence B*H <= 65535 (the step 2^24 - 1), B*H*n <= 2^31.
- * Outputs must not overlap inputs, but where it is said that they may. */
+ * Softmax attention, which the paper's hybrid models interleave with LinSimp
+ * layers (Sec. 4), and a gated linear recurrence: linear attention with a decay
+ * per key channel and row.  (The paper's KDA layer is another one: a delta rule,
+ * whose update subtracts what the state already holds for the key.  It is not
+ * built here.)  Both stand behind the conventions above: dense [B, heads, rows, D]
+ * device tensors, 16-byte aligned, the caller's workspace (256-byte aligned),
+ * calls that only enqueue on `stream`, negative statuses.  D is 32, 64 or 128
+ * with LINSIMP_BF16 and 32 or 64 with LINSIMP_F32.  Results are the same bits on
+ * every run of a call.  Sizes: attention B*H <= 2^20, B*H*nq <= 2^30, nk <= 2^30,
+ * and for the backward B*Hkv*nk <= 2^30; recurrence B*H <= 65535 (the step
+ * 2^24 - 1), B*H*n <= 2^31.  Outputs must not overlap inputs, but where it is
+ * said that they may.
+ *
+ * Precision: sums, maxima, decays and carried states are float32.  With
+ * LINSIMP_BF16 the operands of the matrix products are bf16: besides the inputs,
+ * probabilities and their gradients (attention), decayed rows, pair weights and
+ * states where a product reads them (recurrence) are rounded to it, 2^-8 relative
+ * at most each.  With LINSIMP_F32 nothing is rounded to fewer than 32 bits.
+ * Values that are not finite: rows past a sequence's length are never used,
+ * whatever they hold, but an infinity or NaN in a row that exists may reach
+ * earlier rows too, as zero times it, though these do not see it. */
 
 typedef struct {
   int64_t B;       /* batch (sequences)                                       */
@@ -253,8 +265,10 @@ int linsimp_attn_fwd(const linsimp_attn_dims* dims, const void* q, const void* k
                      const int32_t* lens_q, const int32_t* lens_k, void* out, float* lse,
                      void* workspace, size_t workspace_bytes, void* stream);
 
-/* Backward: exact gradient of sum(dout * out), the probabilities recomputed
- * from lse.
+/* Backward: gradient of sum(dout * out), the probabilities recomputed from lse.
+ * The term dout_i . out_i is taken from the stored out: with LINSIMP_BF16 the
+ * rounding of out leaves dq and dk off by 2^-8 of that term's size, which is all
+ * there is of dq in rows that see a single key.
  *   q, k, v, lens_q, lens_k : as passed to the forward;  out, lse : what it wrote
  *   dout : [B, H, nq, D] dtype
  *   dq : [B, H, nq, D];  dk, dv : [B, Hkv, nk, D], summed over the query heads
@@ -269,7 +283,7 @@ int linsimp_attn_bwd(const linsimp_attn_dims* dims, const void* q, const void* k
  * min(pos[b] + 1, nk) tokens in the ring, itself included (a ring of w slots is
  * a window of w tokens; a longer prompt is its last nk tokens, each in slot
  * position mod nk).  Slots that hold no token do not affect the result.
- *   dims : nq = 1, nk = slots, window = 0 (causal is not read)
+ *   dims : nq = 1, nk = slots, window = 0 (causal: 0 or 1, the same result)
  *   q : [B, H, D]   k, v : [B, Hkv, D]   out : [B, H, D]
  *   kcache, vcache : [B, Hkv, nk, D] in/out
  *   pos : [B] int64, not changed (one tensor serves all layers); a negative
@@ -295,8 +309,8 @@ size_t linsimp_glr_workspace_size(const linsimp_glr_dims* dims, int for_backward
  *   S_t = diag(exp(g_t)) S_{t-1} + k_t v_t^T,   out_t = scale S_t^T q_t
  *   q, k, v, g : [B, H, n, D] dtype;  out : [B, H, n, D] dtype, written
  *   g    : logarithm of the decay, <= 0; -inf clears the channel
- *          (values of q, k, v and dout up to 2^16 and of states up to 2^50 leave
- *          room for factors of up to 2^60 inside a call; far larger ones can
+ *          (values of q, scale q, k, v and dout up to 2^16 and of states up to 2^50
+ *          leave room for factors of up to 2^60 inside a call; far larger ones can
  *          overflow where the definition does not)
  *   s0   : [B, H, D, D] float32 state before the first row (rows: key channel),
  *          or NULL (zero);  s1 : the state after the last row, or NULL.  s1 may
@@ -309,7 +323,7 @@ int linsimp_glr_fwd(const linsimp_glr_dims* dims, const void* q, const void* k, 
                     const void* g, const float* s0, const int32_t* lens, void* out, float* s1,
                     void* workspace, size_t workspace_bytes, void* stream);
 
-/* Backward: exact gradient of sum(dout * out) + sum(ds1 * s1); the states are
+/* Backward: gradient of sum(dout * out) + sum(ds1 * s1); the states are
  * recomputed.
  *   q, k, v, g, s0, lens : as passed to the forward;  dout : [B, H, n, D] dtype
  *   ds1 : [B, H, D, D] float32 gradient of the final state, or NULL (zero)

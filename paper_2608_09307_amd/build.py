@@ -39,7 +39,7 @@ FLAGS = [
 # spills 24 at d = m = 128 with it and without; elsewhere the option raised
 # register counts and lowered occupancy, so it stays local).  Attention's key
 # sweep at d = 128 spills no register with it instead of eight: 16 heads of
-# 16384 tokens 2.27 -> 2.08 ms.
+# 16384 tokens 2.27 -> 2.08 ms in one session.
 SOURCE_FLAGS = {"bwd.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"],
                 "attn.hip": ["-mllvm", "-amdgpu-use-amdgpu-trackers"]}
 

@@ -13,6 +13,11 @@
 // operand type there (bf16: 2^-8 relative at most, and the errors average out
 // over the keys); scores, maxima, sums and outputs are float32 until the final
 // store.
+//
+// Times beside the kernels are of a settled clock (it moves with the load for the
+// first 10 to 50 ms of a run, and the times by up to 30% with it); two times with
+// an arrow, or a list of variants, were taken in turn in one session each and
+// compare with each other only.
 #include "attn.h"
 
 #include <math.h>
@@ -210,11 +215,11 @@ struct Online {
 // them as matrix columns with their fragments in registers; keys come in tiles
 // of 64, staged once for the four waves, two tiles in LDS and one on its way.
 // With `ns` > 1 the keys are split over ns workgroups and joined afterwards.
-// Bound by the matrix and the vector pipes together: a score takes an exp, a
-// multiply-add, a sum and half a maximum and half a conversion, as many cycles
-// as its 4 D flops at D = 64.  16 heads of 16384 causal tokens, D = 128: 1.17 ms,
-// 940 TFLOP/s (a square bf16 matrix product of 8192: 1260); 48 heads of 2048,
-// D = 64: 47 us, 550 TFLOP/s.
+// 16 heads of 16384 causal tokens, D = 128: 1.12 ms, 980 TFLOP/s (a square bf16
+// matrix product of 8192: 1340), the matrix pipe 48% and the vector pipe 38% busy;
+// 48 heads of 2048, D = 64: 42.5 us, 610 TFLOP/s, 28% and 43%.  Neither pipe is
+// full: in a wave the scores' product, the maximum, the exps and the second product
+// follow each other, and two or three waves of a SIMD do not fill the gaps.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct FwdCfg {
@@ -380,7 +385,8 @@ __global__ __launch_bounds__(256) void k_attn_join(AttnArgs a) {
 // barrier until the four waves (and then the ns workgroups) are joined.  Bound
 // by the cache's bytes: one tile is in LDS and the next in flight in registers.
 // 16 query heads on 4 key heads, 256 sequences in rings of 8192, D = 128: 0.55 ms,
-// 6.0 TB/s; 4 sequences of 64k tokens, 2 key heads: 32 us and 6 to join, 4.2 TB/s.
+// 6.0 TB/s (float32, D = 64: 0.63 ms, 5.3); 4 sequences of 64k tokens, 2 key heads:
+// 30 us, 5.7 TB/s, and 5 to join.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct FewCfg {
@@ -549,8 +555,11 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
 // Rows of up to 64 values take two such tiles at once, so that the exponentials
 // of one run under the products of the other (48 heads of 2048 tokens, D = 64: 67
 // -> 63 us, the key sweep 98 -> 88; at D = 128 there are no registers for it).
-// 16 heads of 16384 causal tokens, D = 128: 1.51 ms, 1090 TFLOP/s, the matrix
-// pipe 59% busy.
+// delta is formed from the stored out, whose rounding to the operand type (bf16:
+// 2^-8 of its terms) is all that dq holds in a row with a single key: the sum over
+// p dP instead would need the whole row before its first ds.
+// 16 heads of 16384 causal tokens, D = 128: 1.45 ms, 1130 TFLOP/s of its three
+// products, the matrix pipe 59% busy, the LDS 50%.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct DqCfg {
@@ -698,9 +707,10 @@ __global__ __launch_bounds__(256) void k_attn_sum(const float* part, T* out0, T*
 // registers; per tile of 32 query rows (of every head that shares the keys)
 //   S = q K^T,  dP = do V^T,  dv^T += do^T P,  dk^T += q^T dS.
 // Each gradient is summed by one wave in a fixed order: no atomics.
-// 16 heads of 16384 causal tokens, D = 128: 2.20 ms, 1000 TFLOP/s, bound by the
-// registers: dk, dv and k take 192 of 256, so v is read from LDS and one wave
-// has no second tile to overlap.
+// 16 heads of 16384 causal tokens, D = 128: 2.14 ms, 1030 TFLOP/s of its four
+// products, the matrix pipe 48% busy.  The LDS is the busiest unit, 55% with 22% of
+// that bank conflicts: dk, dv and k take 192 of 256 registers, so v is read from it
+// for every tile.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 struct KvCfg {

@@ -31,6 +31,11 @@
 // at most); the state, all sums and the decays are float32.  Where a float32
 // state is an output, the rows that it sums keep a second bf16 term, so that
 // it is off by 2^-17 of its terms at most.
+//
+// Times beside the kernels are of a settled clock (it moves with the load for the
+// first 10 to 50 ms of a run, and the times by up to 30% with it); two times with
+// an arrow, or a list of variants, were taken in turn in one session each and
+// compare with each other only.
 #include "glr.h"
 
 #include <type_traits>
@@ -443,9 +448,9 @@ template <typename T, int NT> LS_DEV f32x16 rows_by_rows(int h, const T* arow, c
 // Forward.  One wave per 32 value channels (columns of S, all key rows in
 // registers); wave w also scales the 32 key channels w for all waves.  One
 // barrier per chunk, two sets of scaled rows, the next chunk's rows in flight.
-// 32 heads of 16384 tokens, D = 128, 16 segments a head: 175 us, 3.9 TB/s
-// (more than half of a chunk is the wait for its rows), after 97 us for the
-// segments' parts (4.1 TB/s) and 11 for their scan; whole heads at once instead
+// 32 heads of 16384 tokens, D = 128, 16 segments a head: 164 us, 4.3 TB/s
+// (more than half of a chunk is the wait for its rows), after 92 us for the
+// segments' parts (4.5 TB/s) and 11 for their scan; whole heads at once instead
 // leave seven eighths of the CUs idle: 1450 us.
 // ---------------------------------------------------------------------------
 template <typename T, int D> struct GlrFwd {
@@ -632,7 +637,7 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 // every chunk (S_start on the exact way) as operand fragments for the backward,
 // which adds what the segment's start state, decayed by `pre`, contributes; a
 // single segment starts from s0 itself.  Bound by memory: both walks of 32 heads
-// of 16384 tokens, D = 128, with every chunk's 32 KB of Z written: 250 us, 5.3 TB/s.
+// of 16384 tokens, D = 128, with every chunk's 32 KB of Z written: 247 us, 5.4 TB/s.
 // ---------------------------------------------------------------------------
 template <typename T, int D> struct GlrWalk {
   static constexpr int NW = D / 32, NT = 64 * NW;
@@ -822,10 +827,13 @@ LS_DEV float rows_from(float x) {
 // every pair adds to the rows it spans and cancels before them, with the same
 // rounded factors on both sides, so nothing is left of it there; the pairs of a
 // row with itself are left out of c and added to dq and dk apart.
-// 32 heads of 16384 tokens, D = 128: 490 us, 3.6 TB/s (Z is a third of the bytes).
+// 32 heads of 16384 tokens, D = 128: 444 us, 4.0 TB/s (Z is a third of the bytes).
 // Both kinds of wave work on one chunk between two barriers and hold 256
-// registers, two waves on a SIMD; the vector pipe is 38% and the matrix pipe 17%
-// busy, the rest is the chain from a chunk's gates to its gradients.
+// registers, two waves on a SIMD; the vector pipe is 37% and the matrix pipe 16%
+// busy, the rest is the chain from a chunk's gates to its gradients.  The exact
+// instance at D = 128 keeps 260 to 288 of its registers in scratch memory, the
+// forward's 161: with resets in every chunk the same case takes 2.0 ms backward
+// and 0.56 forward.
 // ---------------------------------------------------------------------------
 template <typename T, int D, bool LOW> struct GlrBwd {
   static constexpr int NW = D / 32, NT = 128 * NW;
@@ -1269,7 +1277,7 @@ __global__ __launch_bounds__(4 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 // ---------------------------------------------------------------------------
 // Single-token step: one workgroup per (sequence, head); the state is read and
 // written once, 16 bytes per thread, all of a thread's rows in flight.  Bound by
-// those bytes: 4096 states of 128 x 128: 86 us, 6.3 TB/s.
+// those bytes: 4096 states of 128 x 128: 84 us, 6.4 TB/s.
 // ---------------------------------------------------------------------------
 template <typename T, int D>
 __global__ __launch_bounds__(256) void k_glr_step(const T* q, const T* k, const T* v, const T* g, float* state, T* out, float scale) {

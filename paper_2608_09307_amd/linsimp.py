@@ -495,7 +495,7 @@ def feature_bank(gauss, radii, m, sign_correct=True, omega=None):
 
 
 # ---------------------------------------------------------------------------
-# The mixers a LinSimp stack interleaves with (include/linsimp.h)
+# Softmax attention and the gated linear recurrence (include/linsimp.h)
 # ---------------------------------------------------------------------------
 
 def alloc_bytes(nbytes: int, device) -> torch.Tensor:
