@@ -71,6 +71,22 @@ LS_DEV void tile_and_head(int nt, int heads, bool late_first, int& tile, int& he
   tile = late_first ? nt - 1 - t : t;
 }
 
+// Workgroup -> (32 columns, part of a key head's keys).  The `ncg` workgroups that read
+// the same keys run one after the other, with a multiple of eight parts on one XCD, so
+// that the keys come from its L2 (512 sequences, 16 heads on 4, 32 queries, 512 keys,
+// D = 128: 423 -> 214 us against all parts of one set of columns after the other).
+LS_DEV void cols_and_part(int ncg, int parts, int& cg, int& part) {
+  const int lin = (int)blockIdx.x;
+  if (parts % 8 == 0) {
+    const int slot = lin >> 3;
+    cg = slot % ncg;
+    part = (slot / ncg) * 8 + (lin & 7);
+  } else {
+    cg = lin % ncg;
+    part = lin / ncg;
+  }
+}
+
 // Row padding of the backward's tiles, which are read by rows and transposed: a
 // pitch of 80 or 208 bytes modulo 256 (16 heads of 16k tokens, D = 128: key sweep
 // 2.38 -> 2.20 ms, query sweep 1.57 -> 1.51 against tr_pad's pitch, at which the
@@ -435,9 +451,12 @@ __global__ __launch_bounds__(256) __attribute__((amdgpu_waves_per_eu(2))) void k
   static_assert(C::BYTES <= 80 * 1024, "two workgroups per CU");
   __shared__ __align__(16) char smem[C::BYTES];
   const int tid = threadIdx.x, l = tid & 63, col = l & 31, h = l >> 5, wv = uniform(tid >> 6);
-  const int sp = blockIdx.x % a.ns, bk = blockIdx.x / a.ns, cg = blockIdx.y;
+  const int ncol = a.G * a.nq, ncg = (ncol + 31) / 32;
+  int cg, part;
+  cols_and_part(ncg, a.B * a.Hkv * a.ns, cg, part);
+  const int sp = part % a.ns, bk = part / a.ns;
   const int b = bk / a.Hkv, kh = bk % a.Hkv;
-  const int c = cg * 32 + col, ncol = a.G * a.nq, cc = min(c, ncol - 1);
+  const int c = cg * 32 + col, cc = min(c, ncol - 1);
   const int qh = kh * a.G + cc / a.nq, qi = cc % a.nq;
   const size_t qrow = ((size_t)b * a.H + qh) * a.nq + qi;
   T* sK = (T*)(smem + wv * C::WAVE);
@@ -896,13 +915,14 @@ static int launch_status(const char* what) {
 // Whether the few-row kernel runs (the step has no other), and so which time model
 // the splits come from.  It reads a key head's keys once per 32 columns, the tiled
 // kernel once per head and 128 queries: up to 32 queries of a head never more often.
-// Microseconds, tiled / few-row, at G heads on a key head:
-//   64 sequences, 4 key heads, G = 4, 2048 keys, D = 128:  nq = 12: 153/81, 24: 152/121,
-//     32: 152/156, 48: 154/234;  D = 64: 94/28, 94/48, 94/69, 98/102
-//   4 sequences, 2 key heads, G = 8, 65536 keys, D = 128:  nq = 6: 318/76, 32: 320/150
-//   16 sequences, 8 heads, G = 1, 4096 keys, D = 128:  nq = 32: 52/48, 48: 52/43, 96: 67/109
-// (the last condition: column groups are the grid's second dimension)
-bool attn_few(const AttnShape& s) { return s.nq <= 32 && s.H / s.Hkv * s.nq <= 32 * 65535; }
+// Microseconds, tiled / few-row, at G heads on a key head, D = 128:
+//   256 sequences, 4 key heads, G = 4, 64, 512 and 2048 keys:  nq = 32: 44/44, 167/108,
+//     575/339;  48: 49/61, 181/150, 593/457;  96: -, 204/283, 655/828
+//   256 sequences, 16 heads, G = 1, the same:  nq = 32: 43/45, 217/207, 747/756;
+//     40: 47/79, 228/235, 752/782
+//   4 sequences, 2 key heads, G = 8, 65536 keys:  nq = 6: 307/56, 32: 312/145
+// Above 32 it would still win where many heads share long keys and lose elsewhere.
+bool attn_few(const AttnShape& s) { return s.nq <= 32; }
 
 // Workgroups that share one query tile's (or key head's) keys, from the time in
 // microseconds: the longest workgroup's key tiles and the whole load at the rate
@@ -958,7 +978,7 @@ static int run_fwd(const AttnShape& s, AttnArgs a, hipStream_t st) {
   const char* what = a.pos != nullptr ? "attn step" : "attn forward";
   (void)hipGetLastError();
   if (attn_few(s)) {
-    const dim3 grid((unsigned)(s.B * s.Hkv * a.ns), (unsigned)((a.G * a.nq + 31) / 32));
+    const unsigned grid = (unsigned)(s.B * s.Hkv * a.ns * ((a.G * a.nq + 31) / 32));
     ProfScope ps(a.pos != nullptr ? "attn_step" : "attn_few", st);
     if (a.pos != nullptr) k_attn_few<T, D, true><<<grid, 256, 0, st>>>(a);
     else k_attn_few<T, D, false><<<grid, 256, 0, st>>>(a);
