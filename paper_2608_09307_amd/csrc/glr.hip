@@ -636,7 +636,8 @@ __global__ __launch_bounds__(2 * D) __attribute__((amdgpu_waves_per_eu(2))) void
 // From zero, to the segment's own part and the decay across it.  STORE: also Z of
 // every chunk (S_start on the exact way) as operand fragments for the backward,
 // which adds what the segment's start state, decayed by `pre`, contributes; a
-// single segment starts from s0 itself.  Bound by memory: both walks of 32 heads
+// single segment starts from s0 itself.  (The state is carried in float32; what is
+// stored is rounded as the product that reads it would round it.)  Bound by memory: both walks of 32 heads
 // of 16384 tokens, D = 128, with every chunk's 32 KB of Z written: 247 us, 5.4 TB/s.
 // ---------------------------------------------------------------------------
 template <typename T, int D> struct GlrWalk {
